@@ -279,6 +279,68 @@ int stb_quantize(const void *W, size_t ldw, const double *xnorm, int n, int m, i
 int stb_weight_sumsq(const void *W, int n, int m, size_t ldw, double *sumsq, void *stream);
 int stb_allocate_nm(const double *sumsq, int layers, double r_target, int *N_out);
 
+/* ---- beside and between the structured-binary layers ------------------------------------------------------------------
+ * What a decoder block needs besides them: the linear layers that stay at 8 bits, and the norms.  (The paper binarizes every
+ * linear of a block, Section 3; it leaves the head and the norms as they are.)  Inference only, like the rest of the library.
+ *
+ * Rows in 8 bits, one scale per row: scale[r] = max_j |v[r][j]| / 127 (fp32, rounded to nearest), q[r][j] = the whole number nearest to
+ * 127 v[r][j] / max_j |v[r][j]|, ties to even, as in exact arithmetic.  v = x (fp16, bf16 or fp32), or, with x2, the gated activation
+ * silu(x) x2 = x / (1 + exp(-x)) x2 rounded to fp32 and from there to the 16-bit type of x and x2 (fp16 or bf16 only).  Activations (a row is a
+ * token) and weights (a row is an output channel) alike.  A row without anything but zeros, or whose largest magnitude is below 2^-118,
+ * becomes zeros with scale 0; one with an infinity or a NaN becomes zeros with scale NaN, so that every product with it is NaN.
+ * x: [rows][ldx]; x2: [rows][ldx2]; q: [rows][ldq] (what lies behind the m-th value of a row is left as it is); leading dimensions >= m, in elements.  Any alignment
+ * of x, x2 and q is taken; 16-byte rows (q: 8-byte) are the fast case.  One launch. */
+int stb_quantize_i8(const void *x, size_t ldx, const void *x2, size_t ldx2, stb_dtype xdt, int rows, int m, int8_t *q, size_t ldq,
+                    float *scale, void *stream);
+
+/* The linear layer in 8 bits:  Y[t][i] = x_scale[t] w_scale[i] sum_j W[i][j] X[t][j] (+ bias[i]).  The sum is exact (int32; m <= 131071, else
+ * STB_ERR_SHAPE), rounded to fp32, multiplied by x_scale[t], then by w_scale[i], then the bias is added, each in fp32, and the result is rounded
+ * once to Y's type: every form of the kernel gives the same bits.  W: int8 [n][ldw], X: int8 [T][ldx]; n, m, T of any size from 1; ldw, ldx >= m
+ * and multiples of 16, W and X 16-byte aligned (what lies behind the m-th value of a row is not read into the result); w_scale: fp32 [n],
+ * x_scale: fp32 [T], bias: fp32 [n] or NULL; Y: fp32, fp16 or bf16 [T][ldy], ldy >= n.  No workspace.  dev_status: as for stb_gemm. */
+int stb_gemm_i8(const int8_t *W, size_t ldw, const float *w_scale, const float *bias, int n, int m, const int8_t *X, size_t ldx,
+                const float *x_scale, int T, void *Y, stb_dtype ydt, size_t ldy, int *dev_status, void *stream);
+
+typedef enum stb_norm_kind {
+  STB_NORM_RMS = 0,         /* norm(v) = v / sqrt(mean_j v_j^2 + eps) */
+  STB_NORM_LAYER = 1        /* norm(v) = (v - mean) / sqrt(mean_j (v_j - mean)^2 + eps) */
+} stb_norm_kind;
+
+/* What stb_block_norm does to every token (HOST struct; pointers to DEVICE memory, NULL = without that part):
+ *   b = x;   if (post) b = norm(b) * post_weight + post_bias;   b = b * gate[t / tokens_per_gate];
+ *   r = resid + alpha * b      -> resid_out
+ *   v = norm(r) * weight + bias -> y (rounded to its type), and / or q, q_scale (v in 8 bits, as stb_quantize_i8 defines it)
+ * in fp32 from the loads to the stores (r enters the second norm unrounded), sums over a row in fp32 in a fixed order. */
+typedef struct stb_norm {
+  int tokens, h;            /* h <= 32768, else STB_ERR_SIZE */
+  stb_norm_kind kind;       /* of both norms */
+  int post;                 /* nonzero: the block's output is normed before it is gated and added */
+  float eps, alpha;
+  const void *x;            /* [tokens][ldx]: the block's output */
+  stb_dtype xdt;
+  size_t ldx;
+  const void *resid;        /* [tokens][ldr] or NULL (r = alpha b) */
+  void *resid_out;          /* [tokens][ldro] or NULL; may be resid itself (ldro = ldr) */
+  stb_dtype rdt;            /* of resid and resid_out */
+  size_t ldr, ldro;
+  const void *post_weight, *post_bias, *weight, *bias;   /* [h] */
+  const void *gate;         /* [ceil(tokens / tokens_per_gate)][ldgate] */
+  stb_dtype wdt;            /* of the five of them */
+  int tokens_per_gate;
+  size_t ldgate;
+  void *y;                  /* [tokens][ldy] */
+  stb_dtype ydt;
+  size_t ldy;
+  int8_t *q;                /* [tokens][ldq] */
+  size_t ldq;
+  float *q_scale;           /* [tokens] */
+} stb_norm;
+
+/* Norms before and after a block, fused with its gate, residual scale and residual sum: one pass over the tokens, one launch.  An output
+ * may be the input of its type with the same leading dimension (resid_out = resid, y = x); otherwise outputs must not overlap anything.
+ * Any alignment is taken; 16-byte rows (q: 8-byte) are the fast case.  (Squares of values beyond 10^19 overflow fp32: such a token is 0 or NaN.) */
+int stb_block_norm(const stb_norm *args, void *stream);
+
 /* Static string for a status code. */
 const char *stb_status_str(int status);
 

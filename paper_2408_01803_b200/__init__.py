@@ -21,12 +21,13 @@ STB_OK, STB_ERR_ARG, STB_ERR_SHAPE, STB_ERR_NM, STB_ERR_SIZE = 0, 1, 2, 3, 4
 STB_ERR_UNSUPPORTED, STB_ERR_CORRUPT, STB_ERR_TIMEOUT, STB_ERR_CUDA = 5, 6, 7, 8
 STB_F16, STB_BF16, STB_F32 = 0, 1, 2
 STB_IN_PLAIN, STB_IN_SILU_MUL = 0, 1
+STB_NORM_RMS, STB_NORM_LAYER = 0, 1
 
 EXPORTS = ["stb_pack_size", "stb_pack", "stb_packed_info", "stb_dequant", "stb_gemv", "stb_gemv_wait_selftest",
            "stb_gemm_workspace", "stb_gemm_workspace_min", "stb_gemm", "stb_gemm_f16_workspace", "stb_gemm_f16", "stb_gemm_noalloc", "stb_layer_stack", "stb_layer_stack_host",
            "stb_layer_stack_resident_workspace", "stb_layer_stack_resident", "stb_layer_stack_resident_host",
            "stb_layer_stack_resident_wait_selftest", "stb_layer_stack_checksum", "stb_quantize_workspace", "stb_quantize", "stb_weight_sumsq",
-           "stb_allocate_nm", "stb_status_str"]
+           "stb_allocate_nm", "stb_quantize_i8", "stb_gemm_i8", "stb_block_norm", "stb_status_str"]
 
 
 class StbError(RuntimeError):
@@ -50,6 +51,15 @@ class _Step(C.Structure):
     _fields_ = [("packed", C.c_void_p), ("n", C.c_int), ("m", C.c_int), ("N", C.c_int),
                 ("inp", C.c_void_p), ("out", C.c_void_p), ("odt", C.c_int), ("batch", C.c_int),
                 ("ldin", C.c_size_t), ("ldout", C.c_size_t), ("in2", C.c_void_p), ("input", C.c_int)]
+
+
+class _Norm(C.Structure):
+    _fields_ = [("tokens", C.c_int), ("h", C.c_int), ("kind", C.c_int), ("post", C.c_int), ("eps", C.c_float), ("alpha", C.c_float),
+                ("x", C.c_void_p), ("xdt", C.c_int), ("ldx", C.c_size_t),
+                ("resid", C.c_void_p), ("resid_out", C.c_void_p), ("rdt", C.c_int), ("ldr", C.c_size_t), ("ldro", C.c_size_t),
+                ("post_weight", C.c_void_p), ("post_bias", C.c_void_p), ("weight", C.c_void_p), ("bias", C.c_void_p),
+                ("gate", C.c_void_p), ("wdt", C.c_int), ("tokens_per_gate", C.c_int), ("ldgate", C.c_size_t),
+                ("y", C.c_void_p), ("ydt", C.c_int), ("ldy", C.c_size_t), ("q", C.c_void_p), ("ldq", C.c_size_t), ("q_scale", C.c_void_p)]
 
 
 def _load():
@@ -81,6 +91,9 @@ def _load():
     lib.stb_quantize.argtypes = [v, z, v, i, i, i, C.c_double, p(_Logical), v, z, v]
     lib.stb_weight_sumsq.argtypes = [v, i, i, z, v, v]
     lib.stb_allocate_nm.argtypes = [p(C.c_double), i, C.c_double, p(i)]
+    lib.stb_quantize_i8.argtypes = [v, z, v, z, i, i, i, v, z, v, v]
+    lib.stb_gemm_i8.argtypes = [v, z, v, v, i, i, v, z, v, i, v, i, z, v, v]
+    lib.stb_block_norm.argtypes = [p(_Norm), v]
     lib.stb_status_str.argtypes = [i]
     lib.stb_status_str.restype = C.c_char_p
     for name in EXPORTS:
@@ -111,6 +124,7 @@ class _PythonForms:
     def __init__(self):
         self.gemv, self.gemm, self.gemm_f16 = _gemv_py, _gemm_py, _gemm_f16_py
         self.layer_stack, self.layer_stack_resident = _layer_stack_py, _layer_stack_resident_py
+        self.quantize_i8, self.gemm_i8, self.block_norm = _quantize_i8_py, _gemm_i8_py, _block_norm_py
 
 
 def _fast():
@@ -122,7 +136,8 @@ def _fast():
         import torch  # noqa: F401  (its libraries first)
         from importlib.machinery import ExtensionFileLoader
         from importlib.util import module_from_spec, spec_from_loader
-        names = ("stb_gemv", "stb_gemm_workspace", "stb_gemm", "stb_gemm_f16_workspace", "stb_gemm_f16", "stb_layer_stack", "stb_layer_stack_resident")
+        names = ("stb_gemv", "stb_gemm_workspace", "stb_gemm", "stb_gemm_f16_workspace", "stb_gemm_f16", "stb_layer_stack", "stb_layer_stack_resident",
+                 "stb_quantize_i8", "stb_gemm_i8", "stb_block_norm")
         entries = [C.cast(getattr(_lib, nm), C.c_void_p).value for nm in names]
         try:
             mod = module_from_spec(spec_from_loader("_stb_bind", ExtensionFileLoader("_stb_bind", BIND_PATH)))
@@ -132,7 +147,8 @@ def _fast():
             warnings.warn("the native host path is not available (%s): run `python -m paper_2408_01803_b200.build`" % e)
             mod = _PythonForms()
         else:
-            mod.start(*entries, _check, _gemv_py, _gemm_py, _gemm_f16_py, _layer_stack_py, _layer_stack_resident_py)
+            mod.start(*entries, _check, _gemv_py, _gemm_py, _gemm_f16_py, _layer_stack_py, _layer_stack_resident_py,
+                      _quantize_i8_py, _gemm_i8_py, _block_norm_py)
         _bind = mod
     return _bind
 
@@ -468,3 +484,175 @@ def quantize(W, xnorm, N, lam=-1.0, stream=None):
            "stb_quantize")
     out.update(n=n, m=m, N=N)
     return out
+
+
+# -- beside and between the structured-binary layers: the 8-bit product, its quantizer, the norms of a block --------------------------------
+def _refuse(bad, where):
+    if bad:
+        raise StbError(STB_ERR_ARG, where)
+
+
+def _dtype(t, where):
+    import torch
+    codes = {torch.float32: STB_F32, torch.float16: STB_F16, torch.bfloat16: STB_BF16}
+    if t not in codes:
+        raise StbError(STB_ERR_UNSUPPORTED, "%s: %s" % (where, t))
+    return codes[t]
+
+
+def _rows(t, like, where):
+    """A matrix with values of a row side by side, on the device of `like`; a vector is a matrix of one row."""
+    _refuse(not t.is_cuda or t.device != like.device, "%s is on %s" % (where, t.device))
+    t2 = t if t.dim() == 2 else t.unsqueeze(0)
+    _refuse(t2.dim() != 2 or (t2.stride(1) != 1 and t2.shape[1] > 1), "%s: rows of values side by side are needed" % where)
+    return t2
+
+
+def _ld(t2, unit=1):
+    """The leading dimension; one row alone has none, whatever its stride says."""
+    return t2.stride(0) if t2.shape[0] > 1 else -(-t2.shape[1] // unit) * unit
+
+
+def _vector(t, count, dtype, like, where):
+    _refuse(t.dim() != 1 or t.shape[0] != count or t.dtype != dtype or t.device != like.device or (t.stride(0) != 1 and count > 1),
+            "%s: %d %s values side by side are needed" % (where, count, dtype))
+    return t
+
+
+def _launch_stream(stream, like):
+    """The stream of a call (that of the tensors' device where none is given)."""
+    import torch
+    return C.c_void_p((stream if stream is not None else torch.cuda.current_stream(like.device)).cuda_stream)
+
+
+def _empty_rows_i8(rows, m, device):
+    """Rows in 8 bits as gemm_i8() takes them: on a stride of whole 16 bytes."""
+    import torch
+    return torch.empty((rows, -(-m // 16) * 16), dtype=torch.int8, device=device)[:, :m]
+
+
+def quantize_i8(x, x2=None, q=None, scale=None, stream=None):
+    """stb_quantize_i8: rows of x (fp16, bf16 or fp32 [rows][m], or one row) in 8 bits -> (q int8 [rows][m], scale fp32 [rows]), x ~ q scale;
+    with x2 the rows of silu(x) * x2 (16-bit types).  Activations and weights alike: a scale per token, a scale per output channel."""
+    return (_bind or _fast()).quantize_i8(x, x2, q, scale, stream)
+
+
+def _quantize_i8_py(x, x2=None, q=None, scale=None, stream=None):
+    import torch
+    xr = _rows(x, x, "quantize_i8: x")
+    rows, m = xr.shape
+    x2r = None
+    if x2 is not None:
+        x2r = _rows(x2, x, "quantize_i8: x2")
+        _refuse(x2r.shape != xr.shape or x2.dtype != x.dtype, "quantize_i8: x2 differs from x in shape or type")
+    code = _dtype(x.dtype, "quantize_i8: x")
+    with torch.cuda.device(x.device):
+        with _on(stream):
+            made = [] if q is not None else [_empty_rows_i8(rows, m, x.device)]
+            made += [] if scale is not None else [torch.empty(rows, dtype=torch.float32, device=x.device)]
+        _result(stream, *made)
+        qr = made[0] if q is None else _rows(q, x, "quantize_i8: q")
+        _refuse(qr.dtype != torch.int8 or qr.shape != xr.shape, "quantize_i8: q")
+        sc = made[-1] if scale is None else _vector(scale, rows, torch.float32, x, "quantize_i8: scale")
+        _check(_lib.stb_quantize_i8(_ptr(xr), _ld(xr), _ptr(x2r), _ld(x2r) if x2r is not None else 0, code, rows, m, _ptr(qr), _ld(qr), _ptr(sc),
+                                    _launch_stream(stream, x)), "stb_quantize_i8")
+    return (q if q is not None else (qr if x.dim() == 2 else qr[0])), sc
+
+
+def gemm_i8(xq, x_scale, wq, w_scale, bias=None, out=None, out_dtype=None, dev_status=None, stream=None):
+    """stb_gemm_i8: the linear layer in 8 bits, y[t][i] = x_scale[t] w_scale[i] sum_j wq[i][j] xq[t][j] (+ bias[i]), from one token to
+    thousands.  xq: int8 [T][m] (or one token), wq: int8 [n][m], both on row strides of whole 16 bytes, as quantize_i8() makes them;
+    scales and bias fp32; y fp32 (default), fp16 or bf16 [T][n]."""
+    return (_bind or _fast()).gemm_i8(xq, x_scale, wq, w_scale, bias, out, out_dtype, dev_status, stream)
+
+
+def _gemm_i8_py(xq, x_scale, wq, w_scale, bias=None, out=None, out_dtype=None, dev_status=None, stream=None):
+    import torch
+    xr, wr = _rows(xq, xq, "gemm_i8: xq"), _rows(wq, xq, "gemm_i8: wq")
+    T, m = xr.shape
+    n = wr.shape[0]
+    _refuse(xq.dtype != torch.int8 or wq.dtype != torch.int8 or wr.shape[1] != m, "gemm_i8: int8 rows of the same length are needed")
+    _vector(x_scale, T, torch.float32, xq, "gemm_i8: x_scale")
+    _vector(w_scale, n, torch.float32, xq, "gemm_i8: w_scale")
+    if bias is not None:
+        _vector(bias, n, torch.float32, xq, "gemm_i8: bias")
+    with torch.cuda.device(xq.device):
+        if out is None:
+            _dtype(out_dtype or torch.float32, "gemm_i8: out_dtype")
+            with _on(stream):
+                made = torch.empty((T, n), dtype=out_dtype or torch.float32, device=xq.device)
+            _result(stream, made)
+        y = made if out is None else _rows(out, xq, "gemm_i8: out")
+        _refuse(y.shape != (T, n), "gemm_i8: out")
+        _check(_lib.stb_gemm_i8(_ptr(wr), _ld(wr, 16), _ptr(w_scale), _ptr(bias), n, m, _ptr(xr), _ld(xr, 16), _ptr(x_scale), T, _ptr(y),
+                                _dtype(y.dtype, "gemm_i8: out"), _ld(y), _ptr(dev_status), _launch_stream(stream, xq)), "stb_gemm_i8")
+    return out if out is not None else (y if xq.dim() == 2 else y[0])
+
+
+def block_norm(x, weight=None, residual=None, bias=None, post=False, post_weight=None, post_bias=None, gate=None, alpha=1.0, kind="rms",
+               eps=1e-5, out=None, out_dtype=None, residual_out=None, stream=None):
+    """stb_block_norm: the norms before and after a block with its gate, residual scale and residual sum.
+
+        b = x;  b = norm(b) * post_weight + post_bias (with `post`, or where one of them is given);  b = b * gate
+        r = residual + alpha * b -> residual_out (a new tensor where a residual is given and none to write to; may be `residual` itself)
+        y = norm(r) * weight + bias -> out
+
+    x, residual: [T][h] (or one token) in fp16, bf16 or fp32; weights, biases [h] and gate of one type; gate: [h], or [G][h] with a row for
+    every T / G tokens (a sequence, a token).  kind: "rms" or "layer".  y's type: that of x, out_dtype, or with torch.int8 rows in 8 bits as
+    quantize_i8() makes them, y = (q, scale).  Returns (y, r)."""
+    return (_bind or _fast()).block_norm(x, weight, residual, bias, post, post_weight, post_bias, gate, alpha, kind, eps, out, out_dtype, residual_out, stream)
+
+
+def _block_norm_py(x, weight=None, residual=None, bias=None, post=False, post_weight=None, post_bias=None, gate=None, alpha=1.0, kind="rms",
+                   eps=1e-5, out=None, out_dtype=None, residual_out=None, stream=None):
+    import torch
+    xr = _rows(x, x, "block_norm: x")
+    T, h = xr.shape
+    kinds = {"rms": STB_NORM_RMS, "layer": STB_NORM_LAYER}
+    if kind not in kinds:
+        raise StbError(STB_ERR_UNSUPPORTED, "block_norm: kind %r" % (kind,))
+    a = _Norm(tokens=T, h=h, kind=kinds[kind], eps=eps, alpha=alpha, x=xr.data_ptr(), xdt=_dtype(x.dtype, "block_norm: x"), ldx=_ld(xr))
+    a.post = int(bool(post) or post_weight is not None or post_bias is not None)
+    wdt = next((t.dtype for t in (weight, bias, post_weight, post_bias, gate) if t is not None), None)
+    if wdt is not None:
+        a.wdt = _dtype(wdt, "block_norm: weight")
+    for name, t in (("weight", weight), ("bias", bias), ("post_weight", post_weight), ("post_bias", post_bias)):
+        if t is not None:
+            setattr(a, name, _vector(t, h, wdt, x, "block_norm: " + name).data_ptr())
+    if gate is not None:
+        g = _rows(gate, x, "block_norm: gate")
+        _refuse(g.dtype != wdt or g.shape[1] != h or g.shape[0] < 1 or T % g.shape[0] != 0, "block_norm: gate")
+        a.gate, a.ldgate, a.tokens_per_gate = g.data_ptr(), _ld(g), max(1, T // g.shape[0])
+    if residual is not None:
+        rr = _rows(residual, x, "block_norm: residual")
+        _refuse(rr.shape != xr.shape, "block_norm: residual")
+        a.resid, a.rdt, a.ldr = rr.data_ptr(), _dtype(residual.dtype, "block_norm: residual"), _ld(rr)
+    if residual_out is not None:
+        ro = _rows(residual_out, x, "block_norm: residual_out")
+        _refuse(ro.shape != xr.shape or (residual is not None and residual_out.dtype != residual.dtype), "block_norm: residual_out")
+        a.resid_out, a.rdt, a.ldro = ro.data_ptr(), _dtype(residual_out.dtype, "block_norm: residual_out"), _ld(ro)
+    with torch.cuda.device(x.device):
+        made, r, y = [], residual_out, out
+        with _on(stream):
+            if residual is not None and residual_out is None:
+                made.append(torch.empty((T, h), dtype=residual.dtype, device=x.device))
+                a.resid_out, a.ldro = made[-1].data_ptr(), h
+                r = made[-1] if residual.dim() == 2 else made[-1][0]
+            if out is None and out_dtype == torch.int8:
+                made += [_empty_rows_i8(T, h, x.device), torch.empty(T, dtype=torch.float32, device=x.device)]
+                y = (made[-2] if x.dim() == 2 else made[-2][0], made[-1])
+            elif out is None:
+                _dtype(out_dtype or x.dtype, "block_norm: out_dtype")
+                made.append(torch.empty((T, h), dtype=out_dtype or x.dtype, device=x.device))
+                y = made[-1] if x.dim() == 2 else made[-1][0]
+        _result(stream, *made)
+        if isinstance(y, (tuple, list)):
+            q = _rows(y[0], x, "block_norm: q")
+            _refuse(q.dtype != torch.int8 or q.shape != xr.shape, "block_norm: q")
+            a.q, a.ldq, a.q_scale = q.data_ptr(), _ld(q), _vector(y[1], T, torch.float32, x, "block_norm: scale").data_ptr()
+        else:
+            yr = _rows(y, x, "block_norm: out")
+            _refuse(yr.shape != xr.shape, "block_norm: out")
+            a.y, a.ydt, a.ldy = yr.data_ptr(), _dtype(y.dtype, "block_norm: out"), _ld(yr)
+        _check(_lib.stb_block_norm(C.byref(a), _launch_stream(stream, x)), "stb_block_norm")
+    return y, r

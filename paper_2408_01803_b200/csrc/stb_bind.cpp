@@ -26,6 +26,9 @@ decltype(&stb_gemm_f16_workspace) f_gemm_f16_workspace;
 decltype(&stb_gemm_f16) f_gemm_f16;
 decltype(&stb_layer_stack) f_layer_stack;
 decltype(&stb_layer_stack_resident) f_layer_stack_resident;
+decltype(&stb_quantize_i8) f_quantize_i8;
+decltype(&stb_gemm_i8) f_gemm_i8;
+decltype(&stb_block_norm) f_block_norm;
 PyObject* on_error;                   // callable(status, where): raises
 PyObject *s_n, *s_m, *s_N, *s_buf, *s_dev_status, *s_cuda_stream;
 
@@ -123,7 +126,7 @@ PyObject* failed(int rc, const char* where) {
 PyObject* wrap(const at::Tensor& t) { return THPVariable_Wrap(t); }
 
 // what the Python forms are called with where the plain case does not hold
-PyObject* slow[5];
+PyObject* slow[8];
 PyObject* pass_on(int which, PyObject* const* args, Py_ssize_t n) { return PyObject_Vectorcall(slow[which], args, (size_t)n, nullptr); }
 // where torch threw (no device, no memory, a tensor without storage; nothing was launched): the Python form raises what it raises
 PyObject* threw(int which, PyObject* const* args, Py_ssize_t n) {
@@ -245,11 +248,187 @@ PyObject* bind_layer_stack_resident(PyObject*, PyObject* const* a, Py_ssize_t n)
   }
 }
 
-// start(addresses of the seven entry points in the order above, on_error, the five Python forms)
+// -- the 8-bit product, its quantizer and the norms of a block.  Plain cases: matrices with more than one column on one device, outputs made here
+// (everything else goes to the Python form, which says what is wrong with it).
+bool matrix_of(PyObject* o, c10::Device dev, at::Tensor& x) {
+  if (!THPVariable_Check(o)) return false;
+  x = THPVariable_Unpack(o);
+  return x.dim() == 2 && x.size(0) > 0 && x.size(1) > 1 && x.stride(1) == 1 && x.device() == dev && x.size(0) <= 0x7FFFFFFF && x.size(1) <= 0x7FFFFFFF;
+}
+bool first_matrix(PyObject* o, at::Tensor& x) { return THPVariable_Check(o) && THPVariable_Unpack(o).is_cuda() && matrix_of(o, THPVariable_Unpack(o).device(), x); }
+bool vector_of(PyObject* o, int64_t count, at::ScalarType t, c10::Device dev, at::Tensor& v) {
+  if (!THPVariable_Check(o)) return false;
+  v = THPVariable_Unpack(o);
+  return v.dim() == 1 && v.size(0) == count && v.scalar_type() == t && v.device() == dev && (v.stride(0) == 1 || count == 1);
+}
+bool float_type(at::ScalarType t) { return t == at::kFloat || t == at::kHalf || t == at::kBFloat16; }
+size_t ld_of(const at::Tensor& x, int64_t unit = 1) { return (size_t)(x.size(0) > 1 ? x.stride(0) : (x.size(1) + unit - 1) / unit * unit); }
+// the stream argument, or the current stream of the tensors' device
+bool stream_on(PyObject* o, c10::Device dev, void*& s) {
+  if (o != Py_None) return stream_of(o, s);
+  s = c10::cuda::getCurrentCUDAStream(dev.index()).stream();
+  return true;
+}
+at::Tensor make_i8(int64_t rows, int64_t m, const at::Tensor& like, void* s) {
+  const int64_t ld = (m + 15) / 16 * 16;
+  at::Tensor t = make({rows, ld}, like.options().dtype(at::kChar), s, true);
+  return ld == m ? t : t.narrow(1, 0, m);
+}
+PyObject* pair(PyObject* x, PyObject* y) {      // takes both references
+  PyObject* r = x && y ? PyTuple_Pack(2, x, y) : nullptr;
+  Py_XDECREF(x);
+  Py_XDECREF(y);
+  return r;
+}
+
+// quantize_i8(x, x2, q, scale, stream)
+PyObject* bind_quantize_i8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  at::Tensor x, x2;
+  void* s;
+  try {
+    if (n != 5 || a[2] != Py_None || a[3] != Py_None || !first_matrix(a[0], x) || !float_type(x.scalar_type())) return pass_on(5, a, n);
+    const c10::cuda::CUDAGuard guard(x.device());
+    const bool gated = a[1] != Py_None;
+    if (gated && (!matrix_of(a[1], x.device(), x2) || x2.sizes() != x.sizes() || x2.scalar_type() != x.scalar_type())) return pass_on(5, a, n);
+    if (!stream_on(a[4], x.device(), s)) return pass_on(5, a, n);
+    const int64_t rows = x.size(0), m = x.size(1);
+    at::Tensor q = make_i8(rows, m, x, s), scale = make({rows}, x.options().dtype(at::kFloat), s, true);
+    const void *xp = x.data_ptr(), *x2p = gated ? x2.data_ptr() : nullptr;
+    int8_t* qp = static_cast<int8_t*>(q.data_ptr());
+    float* sp = static_cast<float*>(scale.data_ptr());
+    const size_t ldx = ld_of(x), ldx2 = gated ? ld_of(x2) : 0, ldq = ld_of(q);
+    const stb_dtype dt = dtype_code(x.scalar_type());
+    const int rc = unlocked([&] { return f_quantize_i8(xp, ldx, x2p, ldx2, dt, (int)rows, (int)m, qp, ldq, sp, s); });
+    if (rc != STB_OK) return failed(rc, "stb_quantize_i8");
+    return pair(wrap(q), wrap(scale));
+  } catch (const std::exception&) {
+    return threw(5, a, n);
+  }
+}
+
+// gemm_i8(xq, x_scale, wq, w_scale, bias, out, out_dtype, dev_status, stream)
+PyObject* bind_gemm_i8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  at::Tensor x, xs, w, ws, bias, y;
+  void* s;
+  int* st;
+  try {
+    if (n != 9 || !first_matrix(a[0], x) || x.scalar_type() != at::kChar) return pass_on(6, a, n);
+    const c10::Device dev = x.device();
+    const c10::cuda::CUDAGuard guard(dev);
+    if (!matrix_of(a[2], dev, w) || w.scalar_type() != at::kChar || w.size(1) != x.size(1)) return pass_on(6, a, n);
+    const int64_t T = x.size(0), m = x.size(1), rows = w.size(0);
+    if (!vector_of(a[1], T, at::kFloat, dev, xs) || !vector_of(a[3], rows, at::kFloat, dev, ws)) return pass_on(6, a, n);
+    if (a[4] != Py_None && !vector_of(a[4], rows, at::kFloat, dev, bias)) return pass_on(6, a, n);
+    if (!stream_on(a[8], dev, s) || !status_of(a[7], st)) return pass_on(6, a, n);
+    if (a[5] != Py_None) {
+      if (!matrix_of(a[5], dev, y) || !float_type(y.scalar_type()) || y.size(0) != T || y.size(1) != rows) return pass_on(6, a, n);
+    } else {
+      at::ScalarType t = at::kFloat;
+      if (a[6] != Py_None) {
+        if (!THPDtype_Check(a[6])) return pass_on(6, a, n);
+        t = reinterpret_cast<THPDtype*>(a[6])->scalar_type;
+        if (!float_type(t)) return pass_on(6, a, n);
+      }
+      y = make({T, rows}, x.options().dtype(t), s, true);
+    }
+    const int8_t *xp = static_cast<const int8_t*>(x.data_ptr()), *wp = static_cast<const int8_t*>(w.data_ptr());
+    const float *xsp = static_cast<const float*>(xs.data_ptr()), *wsp = static_cast<const float*>(ws.data_ptr());
+    const float* bp = bias.defined() ? static_cast<const float*>(bias.data_ptr()) : nullptr;
+    void* yp = y.data_ptr();
+    const size_t ldx = ld_of(x, 16), ldw = ld_of(w, 16), ldy = ld_of(y);
+    const stb_dtype dt = dtype_code(y.scalar_type());
+    const int rc = unlocked([&] { return f_gemm_i8(wp, ldw, wsp, bp, (int)rows, (int)m, xp, ldx, xsp, (int)T, yp, dt, ldy, st, s); });
+    if (rc != STB_OK) return failed(rc, "stb_gemm_i8");
+    if (a[5] != Py_None) { Py_INCREF(a[5]); return a[5]; }
+    return wrap(y);
+  } catch (const std::exception&) {
+    return threw(6, a, n);
+  }
+}
+
+// block_norm(x, weight, residual, bias, post, post_weight, post_bias, gate, alpha, kind, eps, out, out_dtype, residual_out, stream)
+PyObject* bind_block_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  at::Tensor x, r, ro, y, q, scale, gate, vec[4];
+  void* s;
+  stb_norm args = {};
+  try {
+    if (n != 15 || !first_matrix(a[0], x) || !float_type(x.scalar_type()) || a[11] != Py_None) return pass_on(7, a, n);
+    const c10::Device dev = x.device();
+    const c10::cuda::CUDAGuard guard(dev);
+    const int64_t T = x.size(0), h = x.size(1);
+    args.tokens = (int)T; args.h = (int)h;
+    if (!PyUnicode_Check(a[9]) || !stream_on(a[14], dev, s) || !PyBool_Check(a[4])) return pass_on(7, a, n);
+    if (PyUnicode_CompareWithASCIIString(a[9], "rms") == 0) args.kind = STB_NORM_RMS;
+    else if (PyUnicode_CompareWithASCIIString(a[9], "layer") == 0) args.kind = STB_NORM_LAYER;
+    else return pass_on(7, a, n);
+    args.alpha = (float)PyFloat_AsDouble(a[8]);
+    args.eps = (float)PyFloat_AsDouble(a[10]);
+    if (PyErr_Occurred()) { PyErr_Clear(); return pass_on(7, a, n); }
+    args.x = x.data_ptr(); args.xdt = dtype_code(x.scalar_type()); args.ldx = ld_of(x);
+    // weight, bias, post_weight, post_bias and the gate: one type
+    static const int kVectors[4] = {1, 3, 5, 6};
+    const void** slots[4] = {&args.weight, &args.bias, &args.post_weight, &args.post_bias};
+    at::ScalarType wt = at::kFloat;
+    bool typed = false;
+    auto same_type = [&](at::ScalarType t) {
+      if (!float_type(t) || (typed && t != wt)) return false;
+      wt = t; typed = true;
+      return true;
+    };
+    for (int i = 0; i < 4; ++i) {
+      PyObject* o = a[kVectors[i]];
+      if (o == Py_None) continue;
+      if (!THPVariable_Check(o) || !same_type(THPVariable_Unpack(o).scalar_type()) || !vector_of(o, h, wt, dev, vec[i])) return pass_on(7, a, n);
+      *slots[i] = vec[i].data_ptr();
+    }
+    args.post = a[4] == Py_True || args.post_weight || args.post_bias;
+    if (a[7] != Py_None) {
+      if (!matrix_of(a[7], dev, gate) || !same_type(gate.scalar_type()) || gate.size(1) != h || T % gate.size(0) != 0) return pass_on(7, a, n);
+      args.gate = gate.data_ptr(); args.ldgate = ld_of(gate); args.tokens_per_gate = (int)(T / gate.size(0));
+    }
+    args.wdt = dtype_code(wt);
+    if (a[2] != Py_None) {
+      if (!matrix_of(a[2], dev, r) || r.sizes() != x.sizes() || !float_type(r.scalar_type())) return pass_on(7, a, n);
+      args.resid = r.data_ptr(); args.ldr = ld_of(r); args.rdt = dtype_code(r.scalar_type());
+    }
+    if (a[13] != Py_None) {
+      if (!matrix_of(a[13], dev, ro) || ro.sizes() != x.sizes() || !float_type(ro.scalar_type()) || (r.defined() && ro.scalar_type() != r.scalar_type())) return pass_on(7, a, n);
+      args.rdt = dtype_code(ro.scalar_type());
+    } else if (r.defined()) {
+      ro = make({T, h}, r.options(), s, true);
+    }
+    if (ro.defined()) { args.resid_out = ro.data_ptr(); args.ldro = ld_of(ro); }
+    at::ScalarType yt = x.scalar_type();
+    if (a[12] != Py_None) {
+      if (!THPDtype_Check(a[12])) return pass_on(7, a, n);
+      yt = reinterpret_cast<THPDtype*>(a[12])->scalar_type;
+    }
+    if (yt == at::kChar) {
+      q = make_i8(T, h, x, s);
+      scale = make({T}, x.options().dtype(at::kFloat), s, true);
+      args.q = static_cast<int8_t*>(q.data_ptr()); args.ldq = ld_of(q); args.q_scale = static_cast<float*>(scale.data_ptr());
+    } else {
+      if (!float_type(yt)) return pass_on(7, a, n);
+      y = make({T, h}, x.options().dtype(yt), s, true);
+      args.y = y.data_ptr(); args.ydt = dtype_code(yt); args.ldy = (size_t)h;
+    }
+    const int rc = unlocked([&] { return f_block_norm(&args, s); });
+    if (rc != STB_OK) return failed(rc, "stb_block_norm");
+    PyObject* second = Py_None;
+    if (a[13] != Py_None) second = a[13];
+    if (a[13] != Py_None || !ro.defined()) Py_INCREF(second);
+    else second = wrap(ro);
+    return pair(q.defined() ? pair(wrap(q), wrap(scale)) : wrap(y), second);
+  } catch (const std::exception&) {
+    return threw(7, a, n);
+  }
+}
+
+// start(addresses of the ten entry points in the order above, on_error, the eight Python forms)
 PyObject* bind_start(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n != 13) { PyErr_SetString(PyExc_TypeError, "start takes 13 arguments"); return nullptr; }
-  void* p[7];
-  for (int i = 0; i < 7; ++i) p[i] = PyLong_AsVoidPtr(a[i]);
+  if (n != 19) { PyErr_SetString(PyExc_TypeError, "start takes 19 arguments"); return nullptr; }
+  void* p[10];
+  for (int i = 0; i < 10; ++i) p[i] = PyLong_AsVoidPtr(a[i]);
   if (PyErr_Occurred()) return nullptr;
   f_gemv = reinterpret_cast<decltype(f_gemv)>(p[0]);
   f_gemm_workspace = reinterpret_cast<decltype(f_gemm_workspace)>(p[1]);
@@ -258,15 +437,19 @@ PyObject* bind_start(PyObject*, PyObject* const* a, Py_ssize_t n) {
   f_gemm_f16 = reinterpret_cast<decltype(f_gemm_f16)>(p[4]);
   f_layer_stack = reinterpret_cast<decltype(f_layer_stack)>(p[5]);
   f_layer_stack_resident = reinterpret_cast<decltype(f_layer_stack_resident)>(p[6]);
-  Py_INCREF(a[7]);
-  on_error = a[7];
-  for (int i = 0; i < 5; ++i) { Py_INCREF(a[8 + i]); slow[i] = a[8 + i]; }
+  f_quantize_i8 = reinterpret_cast<decltype(f_quantize_i8)>(p[7]);
+  f_gemm_i8 = reinterpret_cast<decltype(f_gemm_i8)>(p[8]);
+  f_block_norm = reinterpret_cast<decltype(f_block_norm)>(p[9]);
+  Py_INCREF(a[10]);
+  on_error = a[10];
+  for (int i = 0; i < 8; ++i) { Py_INCREF(a[11 + i]); slow[i] = a[11 + i]; }
   Py_RETURN_NONE;
 }
 
 #define FAST(name, fn) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fn)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST("start", bind_start), FAST("gemv", bind_gemv), FAST("gemm", bind_gemm<false>), FAST("gemm_f16", bind_gemm<true>),
-                         FAST("layer_stack", bind_layer_stack), FAST("layer_stack_resident", bind_layer_stack_resident), {nullptr, nullptr, 0, nullptr}};
+                         FAST("layer_stack", bind_layer_stack), FAST("layer_stack_resident", bind_layer_stack_resident),
+                         FAST("quantize_i8", bind_quantize_i8), FAST("gemm_i8", bind_gemm_i8), FAST("block_norm", bind_block_norm), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_stb_bind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
