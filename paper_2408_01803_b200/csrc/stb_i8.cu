@@ -1,6 +1,7 @@
 // stb_gemm_i8: the linear layer in 8 bits, Y[t][i] = x_scale[t] w_scale[i] sum_j W[i][j] X[t][j] (+ bias[i]).
 // The sums are whole numbers in int32, so every order of them, every split of K and every kernel gives the same bits.
 #include <cooperative_groups.h>
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -8,6 +9,7 @@
 
 #include "../../include/stb.h"
 #include "stb_ptx.cuh"
+#include "stb_tcgen05.cuh"
 
 namespace cg = cooperative_groups;
 
@@ -142,11 +144,215 @@ static cudaError_t launch_gemv_i8(const I8Args& a, cudaStream_t s) {
   return cudaLaunchKernelEx(&cfg, gemv_i8_kernel<NB>, a, ksplit);
 }
 
+
+// ---- the 5th-generation tensor cores ------------------------------------------------------------------------------------------------
+// kind::i8 of tcgen05.mma: signed bytes, int32 in tensor memory.  W is the M side (128 rows of a CTA, the lanes of tensor memory), the
+// tokens are the N side, K comes in stages of 128 columns = one swizzled row of 128 bytes: four instructions of K = 32 each.  Both operands arrive by
+// TMA as they lie in memory; what a box has beyond n, m or T is zeros.
+constexpr int kI8M = 128, kI8K = 128;
+constexpr uint32_t kI8StageA = kI8M * kI8K;
+constexpr uint32_t kI8SmemMax = 232448;
+// Instruction descriptor: D int32 (2), A and B signed (1), both K-major.
+__host__ __device__ inline uint32_t i8_idesc(int M, int bn) { return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(bn >> 3) << 17) | ((uint32_t)(M >> 4) << 24); }
+
+template <int kGroup>
+__device__ __forceinline__ void umma_i8(uint32_t d_tmem, uint32_t adesc_lo, uint32_t bdesc_lo, uint32_t desc_hi, uint32_t idesc, uint32_t accumulate) {
+  if (kGroup == 1)
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::i8 [%0], da, db, %4, p;\n\t}"
+                 ::"r"(d_tmem), "r"(adesc_lo), "r"(bdesc_lo), "r"(desc_hi), "r"(idesc), "r"(accumulate) : "memory");
+  else
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
+                 "tcgen05.mma.cta_group::2.kind::i8 [%0], da, db, %4, p;\n\t}"
+                 ::"r"(d_tmem), "r"(adesc_lo), "r"(bdesc_lo), "r"(desc_hi), "r"(idesc), "r"(accumulate) : "memory");
+}
+// the same place in the shared memory of another CTA of the cluster
+__device__ __forceinline__ uint32_t smem_of_rank(uint32_t a, uint32_t rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
+  return r;
+}
+
+// Some tokens (a decode batch, a short prompt): one CTA per 128 channels, `bn` tokens and part of K; the `ks` parts of a tile are a cluster.
+//   warp 0 brings the stages by TMA, warp 1 issues the products (it also owns tensor memory), warps 4 to 7 read the sums out.
+// Every CTA hands the sums of every eighth-of-tokens chunk to the CTA of the cluster that owns the chunk (chunk mod ks), in that one's shared memory,
+// where the ring was; the owner adds them, scales and stores rows of 128 channels.
+struct I8Batch { int ks, per, stages, ttiles, bn, ring, own; uint32_t stage_bytes, tmem; };
+constexpr int kI8BatchThreads = 256;
+constexpr uint32_t kI8BatchRing = 1024;
+constexpr int kI8MaxRing = 12;
+__global__ void __launch_bounds__(kI8BatchThreads, 1)
+gemm_i8_batch_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, const I8Args args, const __grid_constant__ I8Batch sh,
+                     int* dev_status) {
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const int warp = __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const int ks = sh.ks, kz = (int)blockIdx.x % ks, tile = (int)blockIdx.x / ks, tt = tile % sh.ttiles, mt = tile / sh.ttiles;
+  const int s0 = kz * sh.per, count = max(0, min(sh.stages, s0 + sh.per) - s0);
+  const uint32_t sbase = smem_u32(smem), bar_full = sbase, bar_empty = sbase + 8 * kI8MaxRing, bar_accum = sbase + 16 * kI8MaxRing;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 16 * kI8MaxRing + 8);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + 16 * kI8MaxRing + 16);
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < sh.ring; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
+    mbar_init(bar_accum, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_async_smem();
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&wmap) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&xmap) : "memory");
+  }
+  if (warp == 1) tmem_alloc(smem_u32(tmem_slot), sh.tmem);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_d = *tmem_slot;
+  const float *w_scale = args.w_scale, *x_scale = args.x_scale, *bias = args.bias;
+  begin_after(w_scale, x_scale, bias);
+
+  if (warp == 0) {
+    const bool leader = elect_one();
+    int s = 0;
+    uint32_t parity = 1;
+    for (int it = 0; it < count; ++it) {
+      if (!__all_sync(0xFFFFFFFFu, gemm_wait(bar_empty + 8 * s, parity, abort_flag))) break;
+      if (leader) {
+        const uint32_t at = sbase + kI8BatchRing + (uint32_t)s * sh.stage_bytes, full = bar_full + 8 * s;
+        mbar_expect_tx(full, sh.stage_bytes);
+        tma_load_2d(at, &wmap, (s0 + it) * kI8K, mt * kI8M, full);
+        tma_load_2d(at + kI8StageA, &xmap, (s0 + it) * kI8K, tt * sh.bn, full);
+      }
+      __syncwarp();
+      if (++s == sh.ring) { s = 0; parity ^= 1u; }
+    }
+    if (*abort_flag) {       // let copies in flight land before the CTA gives its shared memory up
+      const long long t0 = clock64();
+      while (clock64() - t0 < 200000) {}
+    }
+  } else if (warp == 1) {
+    const bool leader = elect_one();
+    const uint32_t desc_hi = (uint32_t)(umma_desc(0u) >> 32), lo0 = (uint32_t)umma_desc(sbase + kI8BatchRing), idesc = i8_idesc(kI8M, sh.bn);
+    const uint32_t tmem_u = __shfl_sync(0xFFFFFFFFu, tmem_d, 0);
+    int s = 0;
+    uint32_t parity = 0;
+    for (int it = 0; it < count; ++it) {
+      if (!__all_sync(0xFFFFFFFFu, gemm_wait(bar_full + 8 * s, parity, abort_flag))) break;
+      tc_fence_after();
+      const uint32_t a_lo = lo0 + (uint32_t)s * (sh.stage_bytes >> 4), b_lo = a_lo + (kI8StageA >> 4);
+      if (leader) {
+#pragma unroll
+        for (int k = 0; k < kI8K / 32; ++k) umma_i8<1>(tmem_u, a_lo + 2u * k, b_lo + 2u * k, desc_hi, idesc, (it | k) != 0);
+        umma_commit(bar_empty + 8 * s);
+      }
+      __syncwarp();
+      if (++s == sh.ring) { s = 0; parity ^= 1u; }
+    }
+    if (leader) umma_commit(bar_accum);
+    __syncwarp();
+  }
+  // every CTA of the cluster has read its ring to the end before sums are written where it was
+  const bool have = __all_sync(0xFFFFFFFFu, gemm_wait(bar_accum, 0u, abort_flag));
+  if (ks > 1) { cluster_arrive(); cluster_wait(); } else __syncthreads();
+  const uint32_t sums = sbase + kI8BatchRing;                          // [rank][token of the owner][channel]
+  if (warp >= 4 && have) {
+    tc_fence_after();
+    const int row = 32 * (warp - 4) + lane;
+    for (int c0 = 0; c0 < sh.bn; c0 += 32) {
+      uint32_t r[32];
+      if (count > 0) tmem_ld32(tmem_d + ((uint32_t)(32 * (warp - 4)) << 16) + (uint32_t)c0, r);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int chunk = (c0 >> 3) + j;
+        if (chunk * 8 >= sh.bn) break;
+        const uint32_t at = sums + (uint32_t)(((kz * sh.own + chunk / ks) * 8) * kI8M + row) * 4u, to = ks > 1 ? smem_of_rank(at, (uint32_t)(chunk % ks)) : at;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(to + (uint32_t)i * (kI8M * 4u)), "r"(count > 0 ? r[8 * j + i] : 0u) : "memory");
+      }
+    }
+    tc_fence_before();
+  }
+  if (ks > 1) { cluster_arrive(); cluster_wait(); } else __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem_d, sh.tmem);
+  }
+  const int row = threadIdx.x & (kI8M - 1), r = mt * kI8M + row;
+  if (have && r < args.n) {
+    const int* sum = reinterpret_cast<const int*>(smem + kI8BatchRing) + row;
+    const float ws = w_scale[r], b = bias ? bias[r] : 0.0f;
+    for (int lt = threadIdx.x >> 7; lt < 8 * sh.own; lt += kI8BatchThreads / kI8M) {
+      const int local = 8 * ((lt >> 3) * ks + kz) + (lt & 7), tok = tt * sh.bn + local;
+      if (local >= sh.bn || tok >= args.T) break;
+      int v = 0;
+      for (int z = 0; z < ks; ++z) v += sum[(z * sh.own * 8 + lt) * kI8M];
+      i8_store(args.Y, (size_t)tok * args.ldy + r, args.ydt, i8_value(v, x_scale[tok], ws, b, bias != nullptr));
+    }
+  }
+  if (threadIdx.x == 0 && *abort_flag && dev_status) *dev_status = STB_ERR_TIMEOUT;
+}
+
+// Rows of bytes as a tensor map: boxes of 128 columns x `box_rows` rows, swizzled, zeros beyond the matrix.
+static bool i8_map(EncodeTiledFn enc, CUtensorMap* map, const int8_t* p, int rows, int m, size_t ld, int box_rows) {
+  const cuuint64_t dims[2] = {(cuuint64_t)m, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld};
+  const cuuint32_t box[2] = {(cuuint32_t)kI8K, (cuuint32_t)box_rows}, estr[2] = {1, 1};
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t*>(p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+static cudaError_t allow_smem(const void* kernel, bool* done, uint32_t bytes) {      // the shared-memory limit of a kernel is a per-device setting
+  int dev = 0;
+  const cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev >= 0 && dev < 64 && done[dev]) return cudaSuccess;
+  const cudaError_t f = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (f == cudaSuccess && dev >= 0 && dev < 64) done[dev] = true;
+  return f;
+}
+static cudaError_t launch_cluster(const void* kernel, unsigned grid, unsigned cluster, unsigned threads, uint32_t smem, cudaStream_t s, void** params) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = cluster; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+  cfg.attrs = at; cfg.numAttrs = cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelExC(&cfg, kernel, params);
+}
+
+static int launch_i8_batch(const I8Args& a, int* dev_status, cudaStream_t s) {
+  EncodeTiledFn enc = encode_tiled_fn();
+  if (!enc) return STB_ERR_CUDA;
+  I8Batch sh;
+  sh.stages = (a.m + kI8K - 1) / kI8K;
+  const int mtiles = (a.n + kI8M - 1) / kI8M, least = (a.T + 255) / 256;
+  sh.bn = ((a.T + least - 1) / least + 15) / 16 * 16;
+  sh.ttiles = (a.T + sh.bn - 1) / sh.bn;
+  const long long tiles = (long long)mtiles * sh.ttiles;
+  sh.ks = 1;
+  while (sh.ks < 8 && tiles * sh.ks * 2 <= 148 && sh.stages >= 8 * sh.ks) sh.ks *= 2;
+  sh.per = (sh.stages + sh.ks - 1) / sh.ks;
+  sh.stage_bytes = kI8StageA + (uint32_t)sh.bn * kI8K;
+  sh.ring = (int)((kI8SmemMax - kI8BatchRing) / sh.stage_bytes);
+  if (sh.ring > kI8MaxRing) sh.ring = kI8MaxRing;
+  sh.own = (sh.bn / 8 + sh.ks - 1) / sh.ks;
+  sh.tmem = sh.bn <= 32 ? 32 : (sh.bn <= 64 ? 64 : (sh.bn <= 128 ? 128 : 256));
+  const uint32_t sums = (uint32_t)(sh.ks * sh.own * 8) * kI8M * 4u, ring = (uint32_t)sh.ring * sh.stage_bytes;
+  const uint32_t smem = kI8BatchRing + (ring > sums ? ring : sums);
+  CUtensorMap wmap, xmap;
+  if (!i8_map(enc, &wmap, a.W, a.n, a.m, a.ldw, kI8M) || !i8_map(enc, &xmap, a.X, a.T, a.m, a.ldx, sh.bn)) return STB_ERR_ARG;
+  static bool done[64] = {};
+  if (allow_smem(reinterpret_cast<const void*>(gemm_i8_batch_kernel), done, kI8SmemMax) != cudaSuccess) return STB_ERR_CUDA;
+  I8Args args = a;
+  void* params[] = {&wmap, &xmap, &args, &sh, &dev_status};
+  return launch_cluster(reinterpret_cast<const void*>(gemm_i8_batch_kernel), (unsigned)(tiles * sh.ks), (unsigned)sh.ks, kI8BatchThreads, smem, s, params) == cudaSuccess ? STB_OK : STB_ERR_CUDA;
+}
+
 }  // namespace stb
 
 extern "C" int stb_gemm_i8(const int8_t* W, size_t ldw, const float* w_scale, const float* bias, int n, int m, const int8_t* X, size_t ldx,
                            const float* x_scale, int T, void* Y, stb_dtype ydt, size_t ldy, int* dev_status, void* stream) {
-  (void)dev_status;
   if (!W || !w_scale || !X || !x_scale || !Y) return STB_ERR_ARG;
   if (n < 1 || m < 1 || T < 1 || m > 131071) return STB_ERR_SHAPE;
   if (ydt != STB_F32 && ydt != STB_F16 && ydt != STB_BF16) return STB_ERR_UNSUPPORTED;
@@ -157,6 +363,7 @@ extern "C" int stb_gemm_i8(const int8_t* W, size_t ldw, const float* w_scale, co
     return STB_ERR_ARG;
   const stb::I8Args a = {W, X, w_scale, bias, x_scale, Y, ldw, ldx, ldy, n, m, T, ydt};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = T <= 8 ? stb::launch_gemv_i8<1>(a, s) : (T <= 16 ? stb::launch_gemv_i8<2>(a, s) : stb::launch_gemv_i8<4>(a, s));
+  if (T > 16) return stb::launch_i8_batch(a, dev_status, s);
+  const cudaError_t e = T <= 8 ? stb::launch_gemv_i8<1>(a, s) : stb::launch_gemv_i8<2>(a, s);
   return e == cudaSuccess ? STB_OK : STB_ERR_CUDA;
 }
