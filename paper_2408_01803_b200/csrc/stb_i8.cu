@@ -173,13 +173,53 @@ __device__ __forceinline__ uint32_t smem_of_rank(uint32_t a, uint32_t rank) {
   return r;
 }
 
+// Four channels side by side, from `r` on: their scales, and where a token's results go.
+struct I8Channels {
+  float ws[4], b[4];
+  int r;
+  bool whole;             // all four exist and their results can be stored at once
+  __device__ __forceinline__ I8Channels(const I8Args& a, const float* w_scale, const float* bias, int r_) : r(r_) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      ws[e] = r + e < a.n ? w_scale[r + e] : 0.0f;
+      b[e] = bias && r + e < a.n ? bias[r + e] : 0.0f;
+    }
+    const uintptr_t unit = a.ydt == STB_F32 ? 16 : 8;
+    whole = r + 4 <= a.n && a.ldy % 4 == 0 && (reinterpret_cast<uintptr_t>(a.Y) & (unit - 1)) == 0;
+  }
+  __device__ __forceinline__ void store(const I8Args& a, int tok, float xs, const int4& sum) const {
+    const int s[4] = {sum.x, sum.y, sum.z, sum.w};
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = i8_value(s[e], xs, ws[e], b[e], a.bias != nullptr);
+    const size_t at = (size_t)tok * a.ldy + r;
+    if (!whole) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (r + e < a.n) i8_store(a.Y, at + e, a.ydt, v[e]);
+    } else if (a.ydt == STB_F32) {
+      *reinterpret_cast<float4*>(static_cast<float*>(a.Y) + at) = make_float4(v[0], v[1], v[2], v[3]);
+    } else {
+      uint2 w;
+      if (a.ydt == STB_F16) {
+        const __half2 lo = __floats2half2_rn(v[0], v[1]), hi = __floats2half2_rn(v[2], v[3]);
+        w = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+      } else {
+        const __nv_bfloat162 lo = __floats2bfloat162_rn(v[0], v[1]), hi = __floats2bfloat162_rn(v[2], v[3]);
+        w = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+      }
+      *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.Y) + at) = w;
+    }
+  }
+};
+
 // Some tokens (a decode batch, a short prompt): one CTA per 128 channels, `bn` tokens and part of K; the `ks` parts of a tile are a cluster.
 //   warp 0 brings the stages by TMA, warp 1 issues the products (it also owns tensor memory), warps 4 to 7 read the sums out.
 // Every CTA hands the sums of every eighth-of-tokens chunk to the CTA of the cluster that owns the chunk (chunk mod ks), in that one's shared memory,
 // where the ring was; the owner adds them, scales and stores rows of 128 channels.
 struct I8Batch { int ks, per, stages, ttiles, bn, ring, own; uint32_t stage_bytes, tmem; };
 constexpr int kI8BatchThreads = 256;
-constexpr uint32_t kI8BatchRing = 1024;
+constexpr uint32_t kI8BatchScale = 1024, kI8BatchRing = 2048;     // the tokens' scales; the ring
 constexpr int kI8MaxRing = 12;
 __global__ void __launch_bounds__(kI8BatchThreads, 1)
 gemm_i8_batch_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, const I8Args args, const __grid_constant__ I8Batch sh,
@@ -207,6 +247,9 @@ gemm_i8_batch_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_cons
   const uint32_t tmem_d = *tmem_slot;
   const float *w_scale = args.w_scale, *x_scale = args.x_scale, *bias = args.bias;
   begin_after(w_scale, x_scale, bias);
+  if (warp >= 2)
+    for (int i = (int)threadIdx.x - 64; i < sh.bn; i += kI8BatchThreads - 64)
+      reinterpret_cast<float*>(smem + kI8BatchScale)[i] = tt * sh.bn + i < args.T ? x_scale[tt * sh.bn + i] : 0.0f;
 
   if (warp == 0) {
     const bool leader = elect_one();
@@ -275,16 +318,20 @@ gemm_i8_batch_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_cons
     tc_fence_after();
     tmem_dealloc(tmem_d, sh.tmem);
   }
-  const int row = threadIdx.x & (kI8M - 1), r = mt * kI8M + row;
+  // four channels of a token per lane: 16 bytes of sums at a time, one 8- or 16-byte store
+  const int r = mt * kI8M + 4 * lane;
   if (have && r < args.n) {
-    const int* sum = reinterpret_cast<const int*>(smem + kI8BatchRing) + row;
-    const float ws = w_scale[r], b = bias ? bias[r] : 0.0f;
-    for (int lt = threadIdx.x >> 7; lt < 8 * sh.own; lt += kI8BatchThreads / kI8M) {
+    const float* scales = reinterpret_cast<const float*>(smem + kI8BatchScale);
+    const I8Channels ch(args, w_scale, bias, r);
+    for (int lt = warp; lt < 8 * sh.own; lt += kI8BatchThreads / 32) {
       const int local = 8 * ((lt >> 3) * ks + kz) + (lt & 7), tok = tt * sh.bn + local;
       if (local >= sh.bn || tok >= args.T) break;
-      int v = 0;
-      for (int z = 0; z < ks; ++z) v += sum[(z * sh.own * 8 + lt) * kI8M];
-      i8_store(args.Y, (size_t)tok * args.ldy + r, args.ydt, i8_value(v, x_scale[tok], ws, b, bias != nullptr));
+      int4 v = make_int4(0, 0, 0, 0);
+      for (int z = 0; z < ks; ++z) {
+        const int4 p = *reinterpret_cast<const int4*>(smem + kI8BatchRing + (size_t)(z * sh.own * 8 + lt) * (kI8M * 4) + 16 * lane);
+        v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
+      }
+      ch.store(args, tok, scales[local], v);
     }
   }
   if (threadIdx.x == 0 && *abort_flag && dev_status) *dev_status = STB_ERR_TIMEOUT;
@@ -349,6 +396,231 @@ static int launch_i8_batch(const I8Args& a, int* dev_status, cudaStream_t s) {
   return launch_cluster(reinterpret_cast<const void*>(gemm_i8_batch_kernel), (unsigned)(tiles * sh.ks), (unsigned)sh.ks, kI8BatchThreads, smem, s, params) == cudaSuccess ? STB_OK : STB_ERR_CUDA;
 }
 
+// ---- many tokens ----------------------------------------------------------------------------------------------------------------------
+// Two CTAs of a cluster compute a tile of 256 channels x `bn` tokens together (cta_group::2): each holds 128 rows of W and half of the tokens'
+// rows, the first one's issuing lane multiplies for both, and each has the sums of its 128 channels for all tokens in its tensor memory.  The
+// clusters stay for the whole call and take every so-many-th tile (tokens fastest, so that W is read from HBM once); two accumulators of 256 columns,
+// so that a tile is read out while the next one is multiplied.  Per 128 columns of K a CTA fetches 16 KB + bn / 2 rows for 256 x bn x 128
+// multiply-adds of the pair: at bn = 256 64 bytes per clock of the tensor core, what an SM gets from L2.
+//   warp 0 brings the stages, warp 1 issues the products, warps 4 to 7 read the sums out: 32 tokens at a time through shared memory, from where they leave
+//   as rows of 128 channels by TMA (or by plain stores where rows of Y are on no 16-byte boundary).
+struct I8Prefill { int stages, ttiles, tiles, bn, ring, tma_out; uint32_t stage_bytes; };
+constexpr int kI8PrefillThreads = 256, kI8PrefillMaxRing = 10, kI8OutTokens = 32;
+constexpr uint32_t kI8OutBytes = kI8OutTokens * kI8M * 4u;
+constexpr uint32_t kI8PrefillScale = 512, kI8PrefillOut = 2048, kI8PrefillRing = kI8PrefillOut + 2u * kI8OutBytes;      // (a tile's scales: 256 floats)
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {      // the barrier may be the other CTA's
+  asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+               ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void umma_commit_pair(uint32_t bar) {      // arrives on the barrier of both CTAs
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort_flag) {      // gemm_wait for arrivals of the other CTA
+  const long long t0 = clock64();
+  for (;;) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    if (ok) return true;
+    if (*abort_flag) return false;
+    if (clock64() - t0 > kGemmWaitLimit) { *abort_flag = 1; return false; }
+  }
+}
+// the barrier of the warps 4 to 7: whether all of their threads say yes
+__device__ __forceinline__ bool barrier_and(bool yes) {
+  uint32_t all;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(all) : "r"((uint32_t)yes) : "memory");
+  return all != 0;
+}
+__global__ void __launch_bounds__(kI8PrefillThreads, 1)
+gemm_i8_prefill_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap ymap, const I8Args args,
+                       const __grid_constant__ I8Prefill sh, int* dev_status) {
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const int warp = __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const int rank = (int)(blockIdx.x & 1u), first = (int)(blockIdx.x >> 1), step = (int)(gridDim.x >> 1);
+  const uint32_t sbase = smem_u32(smem);
+  const uint32_t bar_full = sbase, bar_empty = bar_full + 8 * kI8PrefillMaxRing, bar_acc_full = bar_empty + 8 * kI8PrefillMaxRing, bar_acc_empty = bar_acc_full + 16;
+  constexpr uint32_t kBars = 8 * (2 * kI8PrefillMaxRing + 4);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + kBars);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + kBars + 8);
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < sh.ring; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(bar_acc_full + 8 * i, 1); mbar_init(bar_acc_empty + 8 * i, 8); }      // (four warps of either CTA)
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_async_smem();
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&wmap) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&xmap) : "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_arrive();                        // both CTAs' barriers are there before either signals the other's
+  cluster_wait();
+  tc_fence_after();
+  const uint32_t tmem_d = *tmem_slot;
+  const float *w_scale = args.w_scale, *x_scale = args.x_scale, *bias = args.bias;
+  begin_after(w_scale, x_scale, bias);
+
+  if (warp == 0) {
+    const bool leader = elect_one();
+    const uint32_t full0 = smem_of_rank(bar_full, 0u);
+    int s = 0;
+    uint32_t parity = 1;
+    bool ok = true;
+    for (int tile = first; tile < sh.tiles && ok; tile += step) {
+      const int wrow = (tile / sh.ttiles) * 2 * kI8M + rank * kI8M, xrow = (tile % sh.ttiles) * sh.bn + rank * (sh.bn >> 1);
+      for (int it = 0; it < sh.stages; ++it) {
+        ok = __all_sync(0xFFFFFFFFu, gemm_wait(bar_empty + 8 * s, parity, abort_flag));
+        if (!ok) break;
+        if (leader) {
+          const uint32_t at = sbase + kI8PrefillRing + (uint32_t)s * sh.stage_bytes;
+          if (rank == 0) mbar_expect_tx(bar_full + 8 * s, 2u * sh.stage_bytes);
+          tma_load_2d_pair(at, &wmap, it * kI8K, wrow, full0 + 8 * s);
+          tma_load_2d_pair(at + kI8StageA, &xmap, it * kI8K, xrow, full0 + 8 * s);
+        }
+        __syncwarp();
+        if (++s == sh.ring) { s = 0; parity ^= 1u; }
+      }
+    }
+    // the first CTA's products signal this one's barriers: all of that has arrived before the CTA may leave
+    for (int i = 0; i < sh.ring && ok; ++i) {
+      ok = __all_sync(0xFFFFFFFFu, gemm_wait(bar_empty + 8 * s, parity, abort_flag));
+      if (++s == sh.ring) { s = 0; parity ^= 1u; }
+    }
+    if (*abort_flag) {       // let copies in flight land before the CTA gives its shared memory up
+      const long long t0 = clock64();
+      while (clock64() - t0 < 200000) {}
+    }
+  } else if (warp == 1 && rank == 0) {
+    const bool leader = elect_one();
+    const uint32_t desc_hi = (uint32_t)(umma_desc(0u) >> 32), lo0 = (uint32_t)umma_desc(sbase + kI8PrefillRing), idesc = i8_idesc(2 * kI8M, sh.bn);
+    const uint32_t tmem_u = __shfl_sync(0xFFFFFFFFu, tmem_d, 0);
+    int s = 0, use = 0;
+    uint32_t parity = 0;
+    bool ok = true;
+    for (int tile = first; tile < sh.tiles && ok; tile += step, ++use) {
+      const int acc = use & 1;
+      ok = __all_sync(0xFFFFFFFFu, mbar_wait_cluster(bar_acc_empty + 8 * acc, ((uint32_t)(use >> 1) & 1u) ^ 1u, abort_flag));
+      if (!ok) break;
+      tc_fence_after();
+      for (int it = 0; it < sh.stages; ++it) {
+        ok = __all_sync(0xFFFFFFFFu, gemm_wait(bar_full + 8 * s, parity, abort_flag));
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t a_lo = lo0 + (uint32_t)s * (sh.stage_bytes >> 4), b_lo = a_lo + (kI8StageA >> 4);
+        if (leader) {
+#pragma unroll
+          for (int k = 0; k < kI8K / 32; ++k) umma_i8<2>(tmem_u + 256u * acc, a_lo + 2u * k, b_lo + 2u * k, desc_hi, idesc, (it | k) != 0);
+          umma_commit_pair(bar_empty + 8 * s);
+        }
+        __syncwarp();
+        if (++s == sh.ring) { s = 0; parity ^= 1u; }
+      }
+      if (leader) umma_commit_pair(bar_acc_full + 8 * acc);      // (also where the loop was left early: the sums are then not used)
+      __syncwarp();
+    }
+  } else if (warp >= 4) {
+    const int q = warp - 4, row = 32 * q + lane, t128 = (int)threadIdx.x - 128;
+    const uint32_t acc_empty0 = smem_of_rank(bar_acc_empty, 0u);
+    const int elem = args.ydt == STB_F32 ? 4 : 2;
+    float* scales = reinterpret_cast<float*>(smem + kI8PrefillScale);
+    int use = 0, buf = 0;
+    for (int tile = first; tile < sh.tiles; tile += step, ++use) {
+      const int acc = use & 1, r0 = (tile / sh.ttiles) * 2 * kI8M + rank * kI8M, r = r0 + row, tok0 = (tile % sh.ttiles) * sh.bn;
+      const float ws = r < args.n ? w_scale[r] : 0.0f, b = bias && r < args.n ? bias[r] : 0.0f;
+      asm volatile("bar.sync 1, 128;" ::: "memory");             // the last tile's scales have been read
+      for (int i = t128; i < sh.bn; i += 128) scales[i] = tok0 + i < args.T ? x_scale[tok0 + i] : 0.0f;
+      if (!barrier_and(gemm_wait(bar_acc_full + 8 * acc, (uint32_t)(use >> 1) & 1u, abort_flag))) break;      // (one verdict for the four warps)
+      tc_fence_after();
+      for (int c0 = 0; c0 < sh.bn; c0 += kI8OutTokens, buf ^= 1) {
+        uint32_t v[32];
+        tmem_ld32(tmem_d + ((uint32_t)(32 * q) << 16) + (uint32_t)(256 * acc + c0), v);
+        const uint32_t out = sbase + kI8PrefillOut + (uint32_t)buf * kI8OutBytes;
+        if (t128 == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");       // the store before last has read this buffer
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < kI8OutTokens; ++i) {
+          const float f = i8_value((int)v[i], scales[c0 + i], ws, b, bias != nullptr);
+          if (elem == 4) asm volatile("st.shared.f32 [%0], %1;" ::"r"(out + (uint32_t)(i * kI8M + row) * 4u), "f"(f) : "memory");
+          else {
+            const uint16_t h = args.ydt == STB_F16 ? __half_as_ushort(__float2half_rn(f)) : __bfloat16_as_ushort(__float2bfloat16_rn(f));
+            asm volatile("st.shared.u16 [%0], %1;" ::"r"(out + (uint32_t)(i * kI8M + row) * 2u), "h"(h) : "memory");
+          }
+        }
+        if (sh.tma_out) fence_async_smem();
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        if (r0 >= args.n || tok0 + c0 >= args.T) continue;
+        if (sh.tma_out) {
+          if (t128 == 0) {
+            asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(&ymap), "r"(out), "r"(r0), "r"(tok0 + c0) : "memory");
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+          }
+        } else if (r < args.n) {
+          for (int i = 0; i < kI8OutTokens && tok0 + c0 + i < args.T; ++i) {
+            const size_t at = (size_t)(tok0 + c0 + i) * args.ldy + r;
+            const uint8_t* p = smem + kI8PrefillOut + (size_t)buf * kI8OutBytes + (size_t)(i * kI8M + row) * elem;
+            if (elem == 4) static_cast<float*>(args.Y)[at] = *reinterpret_cast<const float*>(p);
+            else static_cast<uint16_t*>(args.Y)[at] = *reinterpret_cast<const uint16_t*>(p);
+          }
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(acc_empty0 + 8 * acc);
+    }
+    if (t128 == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_arrive();                        // nobody leaves while the other CTA's products read its operands or its barriers are signalled
+  cluster_wait();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_d), "r"(512) : "memory");
+  }
+  if (threadIdx.x == 0 && *abort_flag && dev_status) *dev_status = STB_ERR_TIMEOUT;
+}
+
+static int launch_i8_prefill(const I8Args& a, int* dev_status, cudaStream_t s) {
+  EncodeTiledFn enc = encode_tiled_fn();
+  if (!enc) return STB_ERR_CUDA;
+  I8Prefill sh;
+  sh.stages = (a.m + kI8K - 1) / kI8K;
+  const int least = (a.T + 255) / 256;
+  sh.bn = ((a.T + least - 1) / least + 31) / 32 * 32;
+  sh.ttiles = (a.T + sh.bn - 1) / sh.bn;
+  const long long tiles = (long long)((a.n + 2 * kI8M - 1) / (2 * kI8M)) * sh.ttiles;
+  if (tiles > 0x7FFFFFFF) return STB_ERR_SHAPE;
+  sh.tiles = (int)tiles;
+  sh.stage_bytes = kI8StageA + (uint32_t)sh.bn * (kI8K / 2);
+  sh.ring = (int)((kI8SmemMax - kI8PrefillRing) / sh.stage_bytes);
+  if (sh.ring > kI8PrefillMaxRing) sh.ring = kI8PrefillMaxRing;
+  const uint32_t smem = kI8PrefillRing + (uint32_t)sh.ring * sh.stage_bytes;
+  CUtensorMap wmap, xmap, ymap = {};
+  if (!i8_map(enc, &wmap, a.W, a.n, a.m, a.ldw, kI8M) || !i8_map(enc, &xmap, a.X, a.T, a.m, a.ldx, sh.bn / 2)) return STB_ERR_ARG;
+  const int elem = a.ydt == STB_F32 ? 4 : 2;
+  sh.tma_out = (a.ldy * (size_t)elem) % 16 == 0 && (reinterpret_cast<uintptr_t>(a.Y) & 15u) == 0;
+  if (sh.tma_out) {
+    const cuuint64_t dims[2] = {(cuuint64_t)a.n, (cuuint64_t)a.T}, strides[1] = {(cuuint64_t)a.ldy * (cuuint64_t)elem};
+    const cuuint32_t box[2] = {(cuuint32_t)kI8M, (cuuint32_t)kI8OutTokens}, estr[2] = {1, 1};
+    const CUtensorMapDataType dt = a.ydt == STB_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : (a.ydt == STB_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16);
+    sh.tma_out = enc(&ymap, dt, 2, a.Y, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  }
+  static bool done[64] = {};
+  if (allow_smem(reinterpret_cast<const void*>(gemm_i8_prefill_kernel), done, kI8SmemMax) != cudaSuccess) return STB_ERR_CUDA;
+  I8Args args = a;
+  void* params[] = {&wmap, &xmap, &ymap, &args, &sh, &dev_status};
+  const int pairs = sh.tiles < 74 ? sh.tiles : 74;
+  return launch_cluster(reinterpret_cast<const void*>(gemm_i8_prefill_kernel), 2u * (unsigned)pairs, 2u, kI8PrefillThreads, smem, s, params) == cudaSuccess ? STB_OK : STB_ERR_CUDA;
+}
+
 }  // namespace stb
 
 extern "C" int stb_gemm_i8(const int8_t* W, size_t ldw, const float* w_scale, const float* bias, int n, int m, const int8_t* X, size_t ldx,
@@ -363,6 +635,7 @@ extern "C" int stb_gemm_i8(const int8_t* W, size_t ldw, const float* w_scale, co
     return STB_ERR_ARG;
   const stb::I8Args a = {W, X, w_scale, bias, x_scale, Y, ldw, ldx, ldy, n, m, T, ydt};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (T > 256 && (long long)((n + 255) / 256) * ((T + 255) / 256) >= 37) return stb::launch_i8_prefill(a, dev_status, s);
   if (T > 16) return stb::launch_i8_batch(a, dev_status, s);
   const cudaError_t e = T <= 8 ? stb::launch_gemv_i8<1>(a, s) : stb::launch_gemv_i8<2>(a, s);
   return e == cudaSuccess ? STB_OK : STB_ERR_CUDA;
