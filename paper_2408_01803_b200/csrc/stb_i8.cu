@@ -5,6 +5,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
+#include <math.h>
 #include <stdint.h>
 
 #include "../../include/stb.h"
@@ -44,67 +45,59 @@ __device__ __forceinline__ uint4 ldg_stream_v4(const void* p) {
   asm("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
   return v;
 }
-// The bytes [at, at + 16) of a row of m, zeros behind its end (nothing there is read).
-__device__ __noinline__ uint4 row_end(const int8_t* row, int at, int m) {
-  uint32_t w[4] = {0, 0, 0, 0};
-  for (int i = 0; i < 16 && at + i < m; ++i) w[i >> 2] |= (uint32_t)(uint8_t)row[at + i] << (8 * (i & 3));
-  return make_uint4(w[0], w[1], w[2], w[3]);
+// the arrival that says only that this CTA has started (cluster_arrive also waits for what it has written)
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+// Asks for a piece of memory to be brought into L2 (16-byte aligned, a multiple of 16 bytes).  It is read by nobody yet: a kernel may ask for
+// what the one before it is still writing.
+__device__ __forceinline__ void prefetch_l2(const void* p, uint32_t bytes) {
+  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
 }
-
-// Few tokens: the weights are read once and the tensor cores take them as they come.  16 rows of W and up to 8 NB tokens per CTA; its
-// eight warps take every eighth 64 columns of the CTA's part of K.  Lane 4 g + t reads 16 bytes at column 16 t of the rows g and g + 8 and of token
-// g: the same columns of both operands are then in the same place of two instructions, which is all that an order of K has to satisfy.
-// The sums of the warps meet in shared memory, those of the `ksplit` CTAs of a cluster in that of its first.
-constexpr int kI8Warps = 8, kI8Rows = 16, kI8Step = 64;
-template <int NB>
+__device__ __forceinline__ void prefetch_l2_box(const CUtensorMap* map, int x, int y) {
+  asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(map), "r"(x), "r"(y) : "memory");
+}
+// A few tokens (up to 8) and few weights: the tensor cores take the weights as they come.  16 rows of W per CTA; its eight warps take every eighth
+// 64 columns of the CTA's part of K.  Lane 4 g + t reads 16 bytes at column 16 t of the rows g and g + 8 and of token g: the same columns of both
+// operands are then in the same place of two instructions, which is all that an order of K has to satisfy (m is a multiple of 16).  The sums of
+// the warps meet in shared memory, those of the `ksplit` CTAs of a cluster in that of its first.
+constexpr int kI8Warps = 8, kI8Rows = 16, kI8Step = 64, kI8FewTokens = 8;
+constexpr int kI8PrefetchRow = 4096;       // bytes of a row asked for ahead: 4096 x 4096, one token, 6.5 -> 5.1 us (1 KB 5.6, 16 KB 5.2)
 __global__ void __launch_bounds__(32 * kI8Warps)
-gemv_i8_kernel(const I8Args args, int ksplit) {
-  __shared__ int part[kI8Warps][NB][4][32];
-  __shared__ int whole[8][NB][4][32];
+gemv_i8_kernel(const I8Args args, int ksplit, int prefetch) {
+  __shared__ int part[kI8Warps][4][32];
+  __shared__ int whole[8][4][32];
   const int8_t *W = args.W, *X = args.X;
   const float *w_scale = args.w_scale, *x_scale = args.x_scale, *bias = args.bias;
-  if (ksplit > 1) cluster_arrive();          // (before a CTA writes into another's shared memory, that one has started)
-  begin_after(W, X, w_scale, x_scale, bias);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int kz = (int)blockIdx.x % ksplit, row0 = (int)(blockIdx.x / ksplit) * kI8Rows, tok0 = (int)blockIdx.y * 8 * NB;
-  const int m = args.m, steps = (m + kI8Step - 1) / kI8Step;
-  const bool r0 = row0 + g < args.n, r1 = row0 + g + 8 < args.n;
-  const int8_t *w0 = W + (size_t)(r0 ? row0 + g : 0) * args.ldw, *w1 = W + (size_t)(r1 ? row0 + g + 8 : 0) * args.ldw;
-  int acc[NB][4];
-#pragma unroll
-  for (int b = 0; b < NB; ++b)
-#pragma unroll
-    for (int k = 0; k < 4; ++k) acc[b][k] = 0;
+  const int kz = (int)blockIdx.x % ksplit, row0 = (int)(blockIdx.x / ksplit) * kI8Rows;
+  const int m = args.m, steps = (m + kI8Step - 1) / kI8Step, per = (steps + ksplit - 1) / ksplit, end = min(steps, (kz + 1) * per);
+  if (ksplit > 1) cluster_arrive_relaxed();  // (before a CTA writes into another's shared memory, that one has started)
+  if (warp == 0 && lane < kI8Rows && row0 + lane < args.n) {      // while what is before this kernel still runs: the weights, into L2
+    const int from = kz * per * kI8Step, bytes = min(min(end * kI8Step, m) - from, prefetch);
+    if (bytes > 0) prefetch_l2(W + (size_t)(row0 + lane) * args.ldw + from, (uint32_t)bytes);
+  }
+  begin_after(W, X, w_scale, x_scale, bias);
+  const bool r0 = row0 + g < args.n, r1 = row0 + g + 8 < args.n, tok = g < args.T;
+  const int8_t *w0 = W + (size_t)(r0 ? row0 + g : 0) * args.ldw, *w1 = W + (size_t)(r1 ? row0 + g + 8 : 0) * args.ldw, *xr = X + (size_t)(tok ? g : 0) * args.ldx;
+  int acc[4] = {0, 0, 0, 0};
   const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll 4
-  for (int s = kz * kI8Warps + warp; s < steps; s += ksplit * kI8Warps) {
+  for (int s = kz * per + warp; s < end; s += kI8Warps) {
     const int at = s * kI8Step + 16 * t;
-    const bool full = at + 16 <= m;
-    const uint4 a0 = !r0 ? zero : (full ? ldg_stream_v4(w0 + at) : row_end(w0, at, m)), a1 = !r1 ? zero : (full ? ldg_stream_v4(w1 + at) : row_end(w1, at, m));
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const int tok = tok0 + 8 * b + g;
-      uint4 x = zero;
-      if (tok < args.T) {
-        const int8_t* xr = X + (size_t)tok * args.ldx;
-        x = full ? ldg_nc_v4(xr + at) : row_end(xr, at, m);
-      }
-      mma_i8(acc[b], a0.x, a1.x, a0.y, a1.y, x.x, x.y);
-      mma_i8(acc[b], a0.z, a1.z, a0.w, a1.w, x.z, x.w);
-    }
+    const bool in = at < m;
+    const uint4 a0 = r0 && in ? ldg_stream_v4(w0 + at) : zero, a1 = r1 && in ? ldg_stream_v4(w1 + at) : zero, x = tok && in ? ldg_nc_v4(xr + at) : zero;
+    mma_i8(acc, a0.x, a1.x, a0.y, a1.y, x.x, x.y);
+    mma_i8(acc, a0.z, a1.z, a0.w, a1.w, x.z, x.w);
   }
 #pragma unroll
-  for (int b = 0; b < NB; ++b)
-#pragma unroll
-    for (int k = 0; k < 4; ++k) part[warp][b][k][lane] = acc[b][k];
+  for (int k = 0; k < 4; ++k) part[warp][k][lane] = acc[k];
   __syncthreads();
   if (ksplit > 1) cluster_wait();
-  for (int i = threadIdx.x; i < NB * 128; i += 32 * kI8Warps) {
+  const int i = threadIdx.x;
+  if (i < 128) {
     int sum = 0;
 #pragma unroll
-    for (int w = 0; w < kI8Warps; ++w) sum += part[w][i >> 7][(i >> 5) & 3][i & 31];
-    if (ksplit == 1) part[0][i >> 7][(i >> 5) & 3][i & 31] = sum;
-    else cg::this_cluster().map_shared_rank(&whole[0][0][0][0], 0)[(kz * NB * 128) + i] = sum;
+    for (int w = 0; w < kI8Warps; ++w) sum += part[w][i >> 5][i & 31];
+    cg::this_cluster().map_shared_rank(&whole[0][0][0], 0)[kz * 128 + i] = sum;
   }
   if (ksplit > 1) {
     cluster_arrive();
@@ -114,25 +107,28 @@ gemv_i8_kernel(const I8Args args, int ksplit) {
     __syncthreads();
   }
   // accumulator k of lane 4 g + t is row g + 8 (k / 2), token 2 t + k % 2
-  for (int i = threadIdx.x; i < NB * 128; i += 32 * kI8Warps) {
-    const int row = i & 15, tl = i >> 4, tok = tok0 + tl;
-    const int b = tl >> 3, k = ((row >> 3) << 1) | (tl & 1), ln = 4 * (row & 7) + ((tl & 7) >> 1);
-    if (row0 + row >= args.n || tok >= args.T) continue;
+  const int row = i & 15, to = i >> 4, k = ((row >> 3) << 1) | (to & 1), ln = 4 * (row & 7) + ((to & 7) >> 1), r = row0 + row;
+  if (i < 128 && r < args.n && to < args.T) {
     int sum = 0;
-    if (ksplit == 1) sum = part[0][b][k][ln];
-    else for (int z = 0; z < ksplit; ++z) sum += whole[z][b][k][ln];
-    const int r = row0 + row;
-    i8_store(args.Y, (size_t)tok * args.ldy + r, args.ydt, i8_value(sum, x_scale[tok], w_scale[r], bias ? bias[r] : 0.0f, bias != nullptr));
+    for (int z = 0; z < ksplit; ++z) sum += whole[z][k][ln];
+    i8_store(args.Y, (size_t)to * args.ldy + r, args.ydt, i8_value(sum, x_scale[to], w_scale[r], bias ? bias[r] : 0.0f, bias != nullptr));
   }
 }
 
-template <int NB>
-static cudaError_t launch_gemv_i8(const I8Args& a, cudaStream_t s) {
-  const int groups = (a.n + kI8Rows - 1) / kI8Rows, steps = (a.m + kI8Step - 1) / kI8Step;
+// Whether these calls are for gemv_i8_kernel, and the CTAs of a cluster if so (else 0).  Its grid is one wave of up to four CTAs per SM, which gemm_i8_batch_kernel,
+// whose CTAs take longer to set up, cannot beat below some 20 million weights: 1024 x 8192, one token, 3.9 us against 4.7; 4096 x 4096 5.1 against 5.9;
+// 966 x 20352 5.4 against 7.1.  Beyond, bulk copies into deep rings win: 12434 x 1536, eight tokens, 6.7 against 5.8; 11008 x 4096 10.5 against 10.2.
+static int gemv_i8_split(int n, int m, int T) {
+  const int groups = (n + kI8Rows - 1) / kI8Rows, steps = (m + kI8Step - 1) / kI8Step, slots = 4 * 148;
+  if (T > kI8FewTokens || m % 16 != 0 || groups > slots || (long long)n * m > 20000000) return 0;
   int ksplit = 1;
-  while (ksplit < 8 && groups * ksplit < 148 * 2 && steps / (2 * ksplit) >= 2 * kI8Warps) ksplit *= 2;
+  while (ksplit < 8 && groups * ksplit * 2 <= slots && steps >= 10 * ksplit && steps > 16) ksplit *= 2;
+  return ksplit;
+}
+static cudaError_t launch_gemv_i8(const I8Args& a, int ksplit, cudaStream_t s) {
+  const int groups = (a.n + kI8Rows - 1) / kI8Rows;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(groups * ksplit), (unsigned)((a.T + 8 * NB - 1) / (8 * NB)));
+  cfg.gridDim = dim3((unsigned)(groups * ksplit));
   cfg.blockDim = dim3(32 * kI8Warps);
   cfg.stream = s;
   cudaLaunchAttribute at[2];
@@ -141,9 +137,8 @@ static cudaError_t launch_gemv_i8(const I8Args& a, cudaStream_t s) {
   at[1].id = cudaLaunchAttributeClusterDimension;
   at[1].val.clusterDim.x = (unsigned)ksplit; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
   cfg.attrs = at; cfg.numAttrs = ksplit > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, gemv_i8_kernel<NB>, a, ksplit);
+  return cudaLaunchKernelEx(&cfg, gemv_i8_kernel, a, ksplit, kI8PrefetchRow);
 }
-
 
 // ---- the 5th-generation tensor cores ------------------------------------------------------------------------------------------------
 // kind::i8 of tcgen05.mma: signed bytes, int32 in tensor memory.  W is the M side (128 rows of a CTA, the lanes of tensor memory), the
@@ -166,6 +161,23 @@ __device__ __forceinline__ void umma_i8(uint32_t d_tmem, uint32_t adesc_lo, uint
                  "tcgen05.mma.cta_group::2.kind::i8 [%0], da, db, %4, p;\n\t}"
                  ::"r"(d_tmem), "r"(adesc_lo), "r"(bdesc_lo), "r"(desc_hi), "r"(idesc), "r"(accumulate) : "memory");
 }
+// 32 columns of a warp's lanes: asked for, and waited for (all that was asked for; the registers pass through the wait, so that none is used before it)
+__device__ __forceinline__ void tmem_ask32(uint32_t taddr, uint32_t (&r)[32]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+               "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                 "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+                 "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+                 "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+               : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_wait32(uint32_t (&r)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                 "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]),
+                 "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
+                 "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31]) :: "memory");
+}
 // the same place in the shared memory of another CTA of the cluster
 __device__ __forceinline__ uint32_t smem_of_rank(uint32_t a, uint32_t rank) {
   uint32_t r;
@@ -173,61 +185,36 @@ __device__ __forceinline__ uint32_t smem_of_rank(uint32_t a, uint32_t rank) {
   return r;
 }
 
-// Four channels side by side, from `r` on: their scales, and where a token's results go.
-struct I8Channels {
-  float ws[4], b[4];
-  int r;
-  bool whole;             // all four exist and their results can be stored at once
-  __device__ __forceinline__ I8Channels(const I8Args& a, const float* w_scale, const float* bias, int r_) : r(r_) {
+// Results of one channel for up to kCount tokens from `tok` on (`live` of them exist).  The lanes of a warp hold channels side by side.
+template <int kCount>
+__device__ __forceinline__ void i8_channel_out(const I8Args& a, const uint32_t (&sum)[kCount], const float* scales, float ws, float b, bool with_bias, int tok, int live, int r) {
+  const size_t at = (size_t)tok * a.ldy + r;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      ws[e] = r + e < a.n ? w_scale[r + e] : 0.0f;
-      b[e] = bias && r + e < a.n ? bias[r + e] : 0.0f;
-    }
-    const uintptr_t unit = a.ydt == STB_F32 ? 16 : 8;
-    whole = r + 4 <= a.n && a.ldy % 4 == 0 && (reinterpret_cast<uintptr_t>(a.Y) & (unit - 1)) == 0;
+  for (int i = 0; i < kCount; ++i) {
+    if (i >= live) break;
+    const float f = i8_value((int)sum[i], scales[i], ws, b, with_bias);
+    if (a.ydt == STB_F32) static_cast<float*>(a.Y)[at + i * a.ldy] = f;
+    else if (a.ydt == STB_F16) static_cast<__half*>(a.Y)[at + i * a.ldy] = __float2half_rn(f);
+    else static_cast<__nv_bfloat16*>(a.Y)[at + i * a.ldy] = __float2bfloat16_rn(f);
   }
-  __device__ __forceinline__ void store(const I8Args& a, int tok, float xs, const int4& sum) const {
-    const int s[4] = {sum.x, sum.y, sum.z, sum.w};
-    float v[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = i8_value(s[e], xs, ws[e], b[e], a.bias != nullptr);
-    const size_t at = (size_t)tok * a.ldy + r;
-    if (!whole) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (r + e < a.n) i8_store(a.Y, at + e, a.ydt, v[e]);
-    } else if (a.ydt == STB_F32) {
-      *reinterpret_cast<float4*>(static_cast<float*>(a.Y) + at) = make_float4(v[0], v[1], v[2], v[3]);
-    } else {
-      uint2 w;
-      if (a.ydt == STB_F16) {
-        const __half2 lo = __floats2half2_rn(v[0], v[1]), hi = __floats2half2_rn(v[2], v[3]);
-        w = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
-      } else {
-        const __nv_bfloat162 lo = __floats2bfloat162_rn(v[0], v[1]), hi = __floats2bfloat162_rn(v[2], v[3]);
-        w = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
-      }
-      *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.Y) + at) = w;
-    }
-  }
-};
+}
 
 // Some tokens (a decode batch, a short prompt): one CTA per 128 channels, `bn` tokens and part of K; the `ks` parts of a tile are a cluster.
-//   warp 0 brings the stages by TMA, warp 1 issues the products (it also owns tensor memory), warps 4 to 7 read the sums out.
-// Every CTA hands the sums of every eighth-of-tokens chunk to the CTA of the cluster that owns the chunk (chunk mod ks), in that one's shared memory,
-// where the ring was; the owner adds them, scales and stores rows of 128 channels.
-struct I8Batch { int ks, per, stages, ttiles, bn, ring, own; uint32_t stage_bytes, tmem; };
+//   warp 0 brings the stages by TMA, warp 1 issues the products (it also owns tensor memory); then all eight warps read the sums out.
+// ks = 1: straight to Y.  Else eight tokens at a time belong to one CTA of the cluster (group of eight mod ks), which gets everybody's sums of them
+// into its shared memory (32 bytes per channel and CTA), adds, scales and stores.
+struct I8Batch { int lks, per, stages, ttiles, bn, ring, prefetch; uint32_t stage_bytes, tmem; };
 constexpr int kI8BatchThreads = 256;
-constexpr uint32_t kI8BatchScale = 1024, kI8BatchRing = 2048;     // the tokens' scales; the ring
+constexpr uint32_t kI8BatchScale = 1024, kI8BatchRing = 2048;     // the tokens' scales; the ring, and behind it the sums that the CTAs hand over
 constexpr int kI8MaxRing = 12;
 __global__ void __launch_bounds__(kI8BatchThreads, 1)
 gemm_i8_batch_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap xmap, const I8Args args, const __grid_constant__ I8Batch sh,
                      int* dev_status) {
   extern __shared__ __align__(1024) uint8_t smem[];
   const int warp = __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-  const int ks = sh.ks, kz = (int)blockIdx.x % ks, tile = (int)blockIdx.x / ks, tt = tile % sh.ttiles, mt = tile / sh.ttiles;
+  const int lks = sh.lks, ks = 1 << lks, kz = (int)blockIdx.x & (ks - 1), tile = (int)blockIdx.x >> lks, tt = tile % sh.ttiles, mt = tile / sh.ttiles;
   const int s0 = kz * sh.per, count = max(0, min(sh.stages, s0 + sh.per) - s0);
+  if (ks > 1) cluster_arrive_relaxed();    // (before a CTA writes into another's shared memory, that one has started)
   const uint32_t sbase = smem_u32(smem), bar_full = sbase, bar_empty = sbase + 8 * kI8MaxRing, bar_accum = sbase + 16 * kI8MaxRing;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + 16 * kI8MaxRing + 8);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + 16 * kI8MaxRing + 16);
@@ -239,6 +226,8 @@ gemm_i8_batch_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_cons
     fence_async_smem();
     asm volatile("prefetch.tensormap [%0];" ::"l"(&wmap) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&xmap) : "memory");
+    // while what is before this kernel still runs: the first weights, into L2
+    for (int it = 0; it < count && it < sh.prefetch; ++it) prefetch_l2_box(&wmap, (s0 + it) * kI8K, mt * kI8M);
   }
   if (warp == 1) tmem_alloc(smem_u32(tmem_slot), sh.tmem);
   tc_fence_before();
@@ -247,6 +236,8 @@ gemm_i8_batch_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_cons
   const uint32_t tmem_d = *tmem_slot;
   const float *w_scale = args.w_scale, *x_scale = args.x_scale, *bias = args.bias;
   begin_after(w_scale, x_scale, bias);
+  const int row = 32 * (warp & 3) + lane, r = mt * kI8M + row, half = warp >> 2;       // the channel that this thread reads out
+  const float ws = r < args.n ? w_scale[r] : 0.0f, b = bias && r < args.n ? bias[r] : 0.0f;
   if (warp >= 2)
     for (int i = (int)threadIdx.x - 64; i < sh.bn; i += kI8BatchThreads - 64)
       reinterpret_cast<float*>(smem + kI8BatchScale)[i] = tt * sh.bn + i < args.T ? x_scale[tt * sh.bn + i] : 0.0f;
@@ -291,50 +282,124 @@ gemm_i8_batch_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_cons
     if (leader) umma_commit(bar_accum);
     __syncwarp();
   }
-  // every CTA of the cluster has read its ring to the end before sums are written where it was
   const bool have = __all_sync(0xFFFFFFFFu, gemm_wait(bar_accum, 0u, abort_flag));
-  if (ks > 1) { cluster_arrive(); cluster_wait(); } else __syncthreads();
-  const uint32_t sums = sbase + kI8BatchRing;                          // [rank][token of the owner][channel]
-  if (warp >= 4 && have) {
-    tc_fence_after();
-    const int row = 32 * (warp - 4) + lane;
-    for (int c0 = 0; c0 < sh.bn; c0 += 32) {
-      uint32_t r[32];
-      if (count > 0) tmem_ld32(tmem_d + ((uint32_t)(32 * (warp - 4)) << 16) + (uint32_t)c0, r);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int chunk = (c0 >> 3) + j;
-        if (chunk * 8 >= sh.bn) break;
-        const uint32_t at = sums + (uint32_t)(((kz * sh.own + chunk / ks) * 8) * kI8M + row) * 4u, to = ks > 1 ? smem_of_rank(at, (uint32_t)(chunk % ks)) : at;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(to + (uint32_t)i * (kI8M * 4u)), "r"(count > 0 ? r[8 * j + i] : 0u) : "memory");
+  tc_fence_after();
+  const uint32_t from = tmem_d + ((uint32_t)(32 * (warp & 3)) << 16);
+  const float* scales = reinterpret_cast<const float*>(smem + kI8BatchScale);
+  const int live = min(sh.bn, args.T - tt * sh.bn);                    // tokens of the tile
+  if (ks == 1) {
+    __syncthreads();                                                   // (the scales)
+    if (have) {
+      for (int c0 = 32 * half; c0 < live; c0 += 64) {
+        uint32_t v[32];
+        tmem_ask32(from + (uint32_t)c0, v);
+        tmem_wait32(v);
+        if (r < args.n) i8_channel_out<32>(args, v, scales + c0, ws, b, bias != nullptr, tt * sh.bn + c0, live - c0, r);
       }
     }
-    tc_fence_before();
+  } else {
+    cluster_wait();
+    if (have) {
+      const uint32_t mine = sbase + kI8BatchRing + (uint32_t)sh.ring * sh.stage_bytes + (uint32_t)(kz * kI8M) * 32u + (uint32_t)row * 16u;
+      for (int c0 = 32 * half; c0 < live; c0 += 64) {
+        uint32_t v[32];
+        if (count > 0) {
+          tmem_ask32(from + (uint32_t)c0, v);
+          tmem_wait32(v);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] = 0u;                      // (no columns of K were left for this CTA)
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int g = (c0 >> 3) + j;
+          if (8 * g >= live) break;
+          const uint32_t to = smem_of_rank(mine + (uint32_t)((g >> lks << lks) * kI8M) * 32u, (uint32_t)(g & (ks - 1)));
+          asm volatile("st.shared::cluster.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(v[8 * j]), "r"(v[8 * j + 1]), "r"(v[8 * j + 2]), "r"(v[8 * j + 3]) : "memory");
+          asm volatile("st.shared::cluster.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to + 16u * kI8M), "r"(v[8 * j + 4]), "r"(v[8 * j + 5]), "r"(v[8 * j + 6]), "r"(v[8 * j + 7]) : "memory");
+        }
+      }
+    }
+    cluster_arrive();
+    cluster_wait();
+    if (have && r < args.n) {
+      const uint8_t* sums = smem + kI8BatchRing + (size_t)sh.ring * sh.stage_bytes + (size_t)row * 16;
+      for (int g = half * ks + kz; 8 * g < live; g += 2 * ks) {
+        uint32_t v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll 4
+        for (int z = 0; z < ks; ++z) {
+          const uint4* p = reinterpret_cast<const uint4*>(sums + (size_t)((g >> lks << lks) + z) * (kI8M * 32));
+          const uint4 lo = p[0], hi = p[kI8M];
+          v[0] += lo.x; v[1] += lo.y; v[2] += lo.z; v[3] += lo.w; v[4] += hi.x; v[5] += hi.y; v[6] += hi.z; v[7] += hi.w;
+        }
+        i8_channel_out<8>(args, v, scales + 8 * g, ws, b, bias != nullptr, tt * sh.bn + 8 * g, live - 8 * g, r);
+      }
+    }
   }
-  if (ks > 1) { cluster_arrive(); cluster_wait(); } else __syncthreads();
+  tc_fence_before();
+  __syncthreads();
   if (warp == 1) {
     tc_fence_after();
     tmem_dealloc(tmem_d, sh.tmem);
   }
-  // four channels of a token per lane: 16 bytes of sums at a time, one 8- or 16-byte store
-  const int r = mt * kI8M + 4 * lane;
-  if (have && r < args.n) {
-    const float* scales = reinterpret_cast<const float*>(smem + kI8BatchScale);
-    const I8Channels ch(args, w_scale, bias, r);
-    for (int lt = warp; lt < 8 * sh.own; lt += kI8BatchThreads / 32) {
-      const int local = 8 * ((lt >> 3) * ks + kz) + (lt & 7), tok = tt * sh.bn + local;
-      if (local >= sh.bn || tok >= args.T) break;
-      int4 v = make_int4(0, 0, 0, 0);
-      for (int z = 0; z < ks; ++z) {
-        const int4 p = *reinterpret_cast<const int4*>(smem + kI8BatchRing + (size_t)(z * sh.own * 8 + lt) * (kI8M * 4) + 16 * lane);
-        v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
+  if (threadIdx.x == 0 && *abort_flag && dev_status) *dev_status = STB_ERR_TIMEOUT;
+}
+
+// ---- which kernel, which tile ---------------------------------------------------------------------------------------------------------
+// pair: gemm_i8_prefill_kernel.  half: the CTAs of gemm_i8_batch_kernel take half of an SM's shared memory, so that two fit (and the first CTAs of the
+// call after this one can be set up beside the last ones of this one).
+struct I8Plan { bool pair, half; int bn, ttiles, lks; };
+constexpr uint32_t kI8HalfSmem = 115000;
+__host__ inline uint32_t i8_stage_bytes(int bn) { return kI8StageA + (uint32_t)bn * kI8K; }
+__host__ inline uint32_t i8_sum_bytes(int bn, int ks) { return ks > 1 ? (uint32_t)((bn / 8 + ks - 1) / ks * ks) * (kI8M * 32u) : 0u; }
+__host__ inline int i8_ring(int bn, int ks, bool half) {
+  const uint32_t room = half ? kI8HalfSmem : kI8SmemMax, taken = kI8BatchRing + i8_sum_bytes(bn, ks);
+  const int ring = room > taken ? (int)((room - taken) / i8_stage_bytes(bn)) : 0;
+  return ring > kI8MaxRing ? kI8MaxRing : ring;
+}
+// The layout whose estimated time is smallest.  In microseconds, fitted to 4200 timed calls of 450 shapes (n, m of 64 to 28672, T of 1 to 4096); over them the choice
+// is 1.0 % behind the fastest layout of each shape on average, 4 % in one of ten.
+//   gemm_i8_batch_kernel:   a stage of 128 columns 0.12 + 0.0014 bn (0.023 more where two CTAs share an SM), times the stages of the fullest SM; the bytes at
+//                           6.3 TB/s / 0.95, the tokens' rows counting 2.2 times (they are read by every row of tiles); the root of the sum of the two squared;
+//                           1.9 for the call, 0.019 bn per wave for reading the sums out, 0.7 for a cluster's sum, 2.5 per further wave
+//   gemm_i8_prefill_kernel: a stage 0.134 + 0.00053 bn times the stages of a cluster; 2.0 for the call, 0.057 bn for the last tile, 3.1 and 0.0047 bn per further tile
+// A cluster lies within one of the GPU's partitions: of four CTAs 33 fit at once, of eight 15.
+static I8Plan i8_plan(int n, int m, int T) {
+  I8Plan best = {};
+  float best_cost = 3.4e38f;
+  const int stages = (m + kI8K - 1) / kI8K, least = (T + 255) / 256, mtiles = (n + kI8M - 1) / kI8M;
+  const float weights = (float)n * (float)m, tokens = (float)T * (float)m, out = 2.0f * (float)T * (float)n;
+  if (T <= 700) {
+    const float bytes = (weights + 2.2f * tokens + out) * (0.95f / 6.3e6f);
+    for (int tt = least; tt < least + 8; ++tt) {
+      const int bn = ((T + tt - 1) / tt + 15) / 16 * 16;
+      if (bn > 256 || (tt > least && (bn < 48 || (tt - 1) * bn >= T))) continue;
+      for (int lks = 0; lks < 4; ++lks) {
+        const int ks = 1 << lks, one = lks == 0 || lks == 1 ? 148 : (lks == 2 ? 132 : 120);
+        const long long ctas = (long long)mtiles * tt * ks;
+        if (lks > 0 && (stages < 2 * ks || ctas > 600)) break;
+        for (int half = 0; half < 2; ++half) {
+          if (i8_ring(bn, ks, half != 0) < 3) continue;
+          const long long at_once = (long long)one << half, full = ctas / at_once, rest = ctas % at_once;
+          const float per_sm = (float)((full << half) + (rest > one ? 2 : (rest > 0 ? 1 : 0))), waves = (float)(full + (rest > 0));
+          const float sm = per_sm * (float)((stages + ks - 1) / ks) * (0.122f + 0.00137f * (float)bn + (half ? 0.023f : 0.0f));
+          const float cost = 1.93f + sqrtf(sm * sm + bytes * bytes) + 0.0193f * (float)bn * waves + (ks > 1 ? 0.71f + 0.001f * (float)bn : 0.0f) + 2.53f * (waves - 1.0f);
+          if (cost < best_cost) { best_cost = cost; best = {false, half != 0, bn, tt, lks}; }
+        }
       }
-      ch.store(args, tok, scales[local], v);
     }
   }
-  if (threadIdx.x == 0 && *abort_flag && dev_status) *dev_status = STB_ERR_TIMEOUT;
+  if (T > 48) {
+    const float bytes = (weights + tokens + out) * (0.82f / 6.3e6f);
+    for (int tt = least; tt <= (T + 63) / 64; ++tt) {
+      const int bn = ((T + tt - 1) / tt + 31) / 32 * 32;
+      if (bn > 256 || bn < 64 || (tt - 1) * bn >= T) continue;
+      const float turns = (float)(((long long)((mtiles + 1) / 2) * tt + 73) / 74), sm = turns * (float)stages * (0.1336f + 0.000532f * (float)bn);
+      const float cost = 2.0f + sqrtf(sm * sm + bytes * bytes) + 0.0567f * (float)bn + (turns - 1.0f) * (3.07f + 0.0047f * (float)bn);
+      if (cost < best_cost) { best_cost = cost; best = {true, false, bn, tt, 0}; }
+    }
+  }
+  return best;
 }
 
 // Rows of bytes as a tensor map: boxes of 128 columns x `box_rows` rows, swizzled, zeros beyond the matrix.
@@ -368,32 +433,29 @@ static cudaError_t launch_cluster(const void* kernel, unsigned grid, unsigned cl
   return cudaLaunchKernelExC(&cfg, kernel, params);
 }
 
-static int launch_i8_batch(const I8Args& a, int* dev_status, cudaStream_t s) {
+static int launch_i8_batch(const I8Args& a, const I8Plan& plan, int* dev_status, cudaStream_t s) {
   EncodeTiledFn enc = encode_tiled_fn();
   if (!enc) return STB_ERR_CUDA;
   I8Batch sh;
+  const int ks = 1 << plan.lks;
+  sh.lks = plan.lks; sh.bn = plan.bn; sh.ttiles = plan.ttiles;
   sh.stages = (a.m + kI8K - 1) / kI8K;
-  const int mtiles = (a.n + kI8M - 1) / kI8M, least = (a.T + 255) / 256;
-  sh.bn = ((a.T + least - 1) / least + 15) / 16 * 16;
-  sh.ttiles = (a.T + sh.bn - 1) / sh.bn;
-  const long long tiles = (long long)mtiles * sh.ttiles;
-  sh.ks = 1;
-  while (sh.ks < 8 && tiles * sh.ks * 2 <= 148 && sh.stages >= 8 * sh.ks) sh.ks *= 2;
-  sh.per = (sh.stages + sh.ks - 1) / sh.ks;
-  sh.stage_bytes = kI8StageA + (uint32_t)sh.bn * kI8K;
-  sh.ring = (int)((kI8SmemMax - kI8BatchRing) / sh.stage_bytes);
-  if (sh.ring > kI8MaxRing) sh.ring = kI8MaxRing;
-  sh.own = (sh.bn / 8 + sh.ks - 1) / sh.ks;
+  sh.per = (sh.stages + ks - 1) / ks;
+  const long long ctas = (long long)((a.n + kI8M - 1) / kI8M) * sh.ttiles * ks;
+  if (ctas > 0x7FFFFFFF) return STB_ERR_SHAPE;
+  sh.stage_bytes = i8_stage_bytes(sh.bn);
+  const uint32_t sums = i8_sum_bytes(sh.bn, ks);
+  sh.ring = i8_ring(sh.bn, ks, plan.half);
+  sh.prefetch = ctas <= (plan.half ? 296 : 148) ? 4 : 0;       // (a CTA that starts late has nobody to hide behind)
   sh.tmem = sh.bn <= 32 ? 32 : (sh.bn <= 64 ? 64 : (sh.bn <= 128 ? 128 : 256));
-  const uint32_t sums = (uint32_t)(sh.ks * sh.own * 8) * kI8M * 4u, ring = (uint32_t)sh.ring * sh.stage_bytes;
-  const uint32_t smem = kI8BatchRing + (ring > sums ? ring : sums);
+  const uint32_t smem = kI8BatchRing + (uint32_t)sh.ring * sh.stage_bytes + sums;
   CUtensorMap wmap, xmap;
   if (!i8_map(enc, &wmap, a.W, a.n, a.m, a.ldw, kI8M) || !i8_map(enc, &xmap, a.X, a.T, a.m, a.ldx, sh.bn)) return STB_ERR_ARG;
   static bool done[64] = {};
   if (allow_smem(reinterpret_cast<const void*>(gemm_i8_batch_kernel), done, kI8SmemMax) != cudaSuccess) return STB_ERR_CUDA;
   I8Args args = a;
   void* params[] = {&wmap, &xmap, &args, &sh, &dev_status};
-  return launch_cluster(reinterpret_cast<const void*>(gemm_i8_batch_kernel), (unsigned)(tiles * sh.ks), (unsigned)sh.ks, kI8BatchThreads, smem, s, params) == cudaSuccess ? STB_OK : STB_ERR_CUDA;
+  return launch_cluster(reinterpret_cast<const void*>(gemm_i8_batch_kernel), (unsigned)ctas, (unsigned)ks, kI8BatchThreads, smem, s, params) == cudaSuccess ? STB_OK : STB_ERR_CUDA;
 }
 
 // ---- many tokens ----------------------------------------------------------------------------------------------------------------------
@@ -426,6 +488,28 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity,
     if (ok) return true;
     if (*abort_flag) return false;
     if (clock64() - t0 > kGemmWaitLimit) { *abort_flag = 1; return false; }
+  }
+}
+// A channel's results for 32 tokens, into rows of 128 channels in shared memory.
+template <int kType>
+__device__ __forceinline__ void i8_rows_out(const uint32_t (&sum)[32], const float* scales, float ws, float b, bool with_bias, uint32_t out, int row) {
+#pragma unroll
+  for (int i = 0; i < kI8OutTokens; i += 4) {
+    const float4 xs = *reinterpret_cast<const float4*>(scales + i);
+    float f[4] = {i8_value((int)sum[i], xs.x, ws, b, false), i8_value((int)sum[i + 1], xs.y, ws, b, false), i8_value((int)sum[i + 2], xs.z, ws, b, false), i8_value((int)sum[i + 3], xs.w, ws, b, false)};
+    if (with_bias) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f[e] = __fadd_rn(f[e], b);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (kType == STB_F32) {
+        asm volatile("st.shared.f32 [%0], %1;" ::"r"(out + (uint32_t)((i + e) * kI8M + row) * 4u), "f"(f[e]) : "memory");
+      } else {
+        const uint16_t h = kType == STB_F16 ? __half_as_ushort(__float2half_rn(f[e])) : __bfloat16_as_ushort(__float2bfloat16_rn(f[e]));
+        asm volatile("st.shared.u16 [%0], %1;" ::"r"(out + (uint32_t)((i + e) * kI8M + row) * 2u), "h"(h) : "memory");
+      }
+    }
   }
 }
 // the barrier of the warps 4 to 7: whether all of their threads say yes
@@ -538,20 +622,21 @@ gemm_i8_prefill_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_co
       for (int i = t128; i < sh.bn; i += 128) scales[i] = tok0 + i < args.T ? x_scale[tok0 + i] : 0.0f;
       if (!barrier_and(gemm_wait(bar_acc_full + 8 * acc, (uint32_t)(use >> 1) & 1u, abort_flag))) break;      // (one verdict for the four warps)
       tc_fence_after();
+      uint32_t v[2][32];
+      const uint32_t from = tmem_d + ((uint32_t)(32 * q) << 16) + 256u * acc;
+      tmem_ask32(from, v[0]);
+#pragma unroll 2
       for (int c0 = 0; c0 < sh.bn; c0 += kI8OutTokens, buf ^= 1) {
-        uint32_t v[32];
-        tmem_ld32(tmem_d + ((uint32_t)(32 * q) << 16) + (uint32_t)(256 * acc + c0), v);
+        uint32_t(&now)[32] = v[(c0 / kI8OutTokens) & 1];
+        tmem_wait32(now);
+        if (c0 + kI8OutTokens < sh.bn) tmem_ask32(from + (uint32_t)(c0 + kI8OutTokens), v[((c0 / kI8OutTokens) & 1) ^ 1]);
         const uint32_t out = sbase + kI8PrefillOut + (uint32_t)buf * kI8OutBytes;
         if (t128 == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");       // the store before last has read this buffer
         asm volatile("bar.sync 1, 128;" ::: "memory");
-#pragma unroll
-        for (int i = 0; i < kI8OutTokens; ++i) {
-          const float f = i8_value((int)v[i], scales[c0 + i], ws, b, bias != nullptr);
-          if (elem == 4) asm volatile("st.shared.f32 [%0], %1;" ::"r"(out + (uint32_t)(i * kI8M + row) * 4u), "f"(f) : "memory");
-          else {
-            const uint16_t h = args.ydt == STB_F16 ? __half_as_ushort(__float2half_rn(f)) : __bfloat16_as_ushort(__float2bfloat16_rn(f));
-            asm volatile("st.shared.u16 [%0], %1;" ::"r"(out + (uint32_t)(i * kI8M + row) * 2u), "h"(h) : "memory");
-          }
+        switch (args.ydt) {
+          case STB_F32: i8_rows_out<STB_F32>(now, scales + c0, ws, b, bias != nullptr, out, row); break;
+          case STB_F16: i8_rows_out<STB_F16>(now, scales + c0, ws, b, bias != nullptr, out, row); break;
+          default: i8_rows_out<STB_BF16>(now, scales + c0, ws, b, bias != nullptr, out, row); break;
         }
         if (sh.tma_out) fence_async_smem();
         asm volatile("bar.sync 1, 128;" ::: "memory");
@@ -587,14 +672,12 @@ gemm_i8_prefill_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_co
   if (threadIdx.x == 0 && *abort_flag && dev_status) *dev_status = STB_ERR_TIMEOUT;
 }
 
-static int launch_i8_prefill(const I8Args& a, int* dev_status, cudaStream_t s) {
+static int launch_i8_prefill(const I8Args& a, const I8Plan& plan, int* dev_status, cudaStream_t s) {
   EncodeTiledFn enc = encode_tiled_fn();
   if (!enc) return STB_ERR_CUDA;
   I8Prefill sh;
   sh.stages = (a.m + kI8K - 1) / kI8K;
-  const int least = (a.T + 255) / 256;
-  sh.bn = ((a.T + least - 1) / least + 31) / 32 * 32;
-  sh.ttiles = (a.T + sh.bn - 1) / sh.bn;
+  sh.bn = plan.bn; sh.ttiles = plan.ttiles;
   const long long tiles = (long long)((a.n + 2 * kI8M - 1) / (2 * kI8M)) * sh.ttiles;
   if (tiles > 0x7FFFFFFF) return STB_ERR_SHAPE;
   sh.tiles = (int)tiles;
@@ -635,8 +718,7 @@ extern "C" int stb_gemm_i8(const int8_t* W, size_t ldw, const float* w_scale, co
     return STB_ERR_ARG;
   const stb::I8Args a = {W, X, w_scale, bias, x_scale, Y, ldw, ldx, ldy, n, m, T, ydt};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (T > 256 && (long long)((n + 255) / 256) * ((T + 255) / 256) >= 37) return stb::launch_i8_prefill(a, dev_status, s);
-  if (T > 16) return stb::launch_i8_batch(a, dev_status, s);
-  const cudaError_t e = T <= 8 ? stb::launch_gemv_i8<1>(a, s) : stb::launch_gemv_i8<2>(a, s);
-  return e == cudaSuccess ? STB_OK : STB_ERR_CUDA;
+  if (const int ksplit = stb::gemv_i8_split(n, m, T)) return stb::launch_gemv_i8(a, ksplit, s) == cudaSuccess ? STB_OK : STB_ERR_CUDA;
+  const stb::I8Plan plan = stb::i8_plan(n, m, T);
+  return plan.pair ? stb::launch_i8_prefill(a, plan, dev_status, s) : stb::launch_i8_batch(a, plan, dev_status, s);
 }
