@@ -1,9 +1,10 @@
 // Rows between the linears of a decoder block: stb_quantize_i8 (rows in 8 bits, one scale each, the gated activation formed on the way)
 // and stb_block_norm (the norms before and after a block with its gate, residual scale and residual sum).
 //
-// Both are bound by memory: every value is read once, kept in registers as fp32 (8 per thread and piece, up to four pieces), and every
-// output is written once, whatever happens in between.  A row of up to 1024 values belongs to one warp, a longer one to one CTA of up to
-// 1024 threads; row sums and maxima go through shuffles and, per CTA, one barrier each.
+// Both are bound by memory: every value is read once and every output written once, whatever happens in between.  A row of up to 1024 values
+// belongs to one warp, a longer one to one CTA; row sums and maxima go through shuffles and, per CTA, one barrier each.  With many long rows a
+// CTA takes row after row, and the next one's values are on their way into shared memory (cp.async: every thread copies, and reads back, only
+// its own pieces, so that nothing has to be synchronised for them) while this one is reduced and written.
 //
 // 8 bits: s = max|v| / 127, q = the whole number nearest to 127 v / max|v| (ties to even), decided as in exact arithmetic: the product with
 // the rounded reciprocal is within 127 * 2^-22 of the quotient, so only a value that near to a border (one in 10^4) is decided by the exact
@@ -19,16 +20,15 @@
 namespace stb {
 
 constexpr int kPiece = 8;                 // values of a thread in a row, side by side
-constexpr int kMaxPieces = 4;
 constexpr int kMaxRowThreads = 1024;
-constexpr int kMaxRow = kPiece * kMaxPieces * kMaxRowThreads;
+constexpr int kMaxRow = 32768;            // values of a row that fit the registers of a CTA
 constexpr float kSmallestMax = 3.0092655e-36f;      // 2^-118: below it 127 / max would overflow; such a row is zeros with scale 0
 
 __host__ __device__ inline int dtype_bytes(int dt) { return dt == STB_F32 ? 4 : 2; }
 
-// ---- eight values of a row ---------------------------------------------------------------------------------------------------------
-// Where a thread's values of a row lie: piece p of thread `lane` of `width` is the eight values at 8 (p width + lane) where rows may be
-// read in 16-byte pieces, else every value is width behind the one before it, so that a warp's loads stay together.
+// ---- a thread's values of a row ------------------------------------------------------------------------------------------------------
+// Piece p of thread `lane` of `width` is the eight values at 8 (p width + lane) where rows can be read in 16-byte pieces (their length a multiple
+// of 8), else every value is width behind the one before it, so that a warp's loads stay together.
 template <bool kVec>
 struct RowPlace {
   int lane, width, m;
@@ -48,34 +48,6 @@ __device__ __forceinline__ void unpack_two(uint32_t w, int dt, float& a, float& 
     b = __uint_as_float(w & 0xFFFF0000u);
   }
 }
-// v[p][k] = value at(p, k) of the row that starts at `row`, 0 behind its end.  All loads of a row are issued before the first is used.
-template <int P, bool kVec>
-__device__ __forceinline__ void load_row(const RowPlace<kVec>& pl, const void* row, int dt, float (&v)[P][kPiece]) {
-#pragma unroll
-  for (int p = 0; p < P; ++p) {
-    const int i = pl.at(p, 0);
-    if (kVec && i + kPiece <= pl.m) {
-      if (dt == STB_F32) {
-        const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(row) + i);
-        const float4 a = q[0], b = q[1];
-        v[p][0] = a.x; v[p][1] = a.y; v[p][2] = a.z; v[p][3] = a.w; v[p][4] = b.x; v[p][5] = b.y; v[p][6] = b.z; v[p][7] = b.w;
-      } else {
-        const uint4 a = *reinterpret_cast<const uint4*>(static_cast<const unsigned short*>(row) + i);
-        unpack_two(a.x, dt, v[p][0], v[p][1]); unpack_two(a.y, dt, v[p][2], v[p][3]);
-        unpack_two(a.z, dt, v[p][4], v[p][5]); unpack_two(a.w, dt, v[p][6], v[p][7]);
-      }
-    } else {
-#pragma unroll
-      for (int k = 0; k < kPiece; ++k) {
-        const int e = pl.at(p, k);
-        v[p][k] = e < pl.m ? load_one(row, (size_t)e, dt) : 0.0f;
-      }
-    }
-  }
-}
-__device__ __forceinline__ unsigned short to_sixteen(float v, int dt) {
-  return dt == STB_F16 ? __half_as_ushort(__float2half_rn(v)) : __bfloat16_as_ushort(__float2bfloat16_rn(v));
-}
 __device__ __forceinline__ uint32_t pack_two(float a, float b, int dt) {
   if (dt == STB_F16) {
     const __half2 h = __floats2half2_rn(a, b);
@@ -84,12 +56,64 @@ __device__ __forceinline__ uint32_t pack_two(float a, float b, int dt) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
+__device__ __forceinline__ void unpack_piece(const uint4& a, int dt, float (&v)[kPiece]) {
+  unpack_two(a.x, dt, v[0], v[1]); unpack_two(a.y, dt, v[2], v[3]);
+  unpack_two(a.z, dt, v[4], v[5]); unpack_two(a.w, dt, v[6], v[7]);
+}
+__device__ __forceinline__ void floats_piece(const float4& a, const float4& b, float (&v)[kPiece]) {
+  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+// v[p][k] = value at(p, k) of the row that starts at `row`, 0 behind its end.
+template <int P, bool kVec>
+__device__ __forceinline__ void load_row(const RowPlace<kVec>& pl, const void* row, int dt, float (&v)[P][kPiece]) {
+  if (kVec && dt == STB_F32) {
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int i = pl.at(p, 0);
+      float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f), b = a;
+      if (i < pl.m) { const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(row) + i); a = q[0]; b = q[1]; }
+      floats_piece(a, b, v[p]);
+    }
+  } else if (kVec) {
+    uint4 a[P];
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int i = pl.at(p, 0);
+      a[p] = make_uint4(0u, 0u, 0u, 0u);
+      if (i < pl.m) a[p] = *reinterpret_cast<const uint4*>(static_cast<const unsigned short*>(row) + i);
+    }
+#pragma unroll
+    for (int p = 0; p < P; ++p) unpack_piece(a[p], dt, v[p]);
+  } else if (dt == STB_F32) {
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+      for (int k = 0; k < kPiece; ++k) {
+        const int e = pl.at(p, k);
+        v[p][k] = e < pl.m ? static_cast<const float*>(row)[e] : 0.0f;
+      }
+  } else {
+    unsigned short u[P][kPiece];
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+      for (int k = 0; k < kPiece; ++k) {
+        const int e = pl.at(p, k);
+        u[p][k] = e < pl.m ? static_cast<const unsigned short*>(row)[e] : (unsigned short)0;
+      }
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+      for (int k = 0; k < kPiece; k += 2) unpack_two((uint32_t)u[p][k] | ((uint32_t)u[p][k + 1] << 16), dt, v[p][k], v[p][k + 1]);
+  }
+}
 template <int P, bool kVec>
 __device__ __forceinline__ void store_row(const RowPlace<kVec>& pl, void* row, int dt, const float (&v)[P][kPiece]) {
 #pragma unroll
   for (int p = 0; p < P; ++p) {
     const int i = pl.at(p, 0);
-    if (kVec && i + kPiece <= pl.m) {
+    if (kVec) {
+      if (i >= pl.m) break;
       if (dt == STB_F32) {
         float4* q = reinterpret_cast<float4*>(static_cast<float*>(row) + i);
         q[0] = make_float4(v[p][0], v[p][1], v[p][2], v[p][3]);
@@ -99,44 +123,89 @@ __device__ __forceinline__ void store_row(const RowPlace<kVec>& pl, void* row, i
             make_uint4(pack_two(v[p][0], v[p][1], dt), pack_two(v[p][2], v[p][3], dt), pack_two(v[p][4], v[p][5], dt), pack_two(v[p][6], v[p][7], dt));
       }
     } else {
+      if (dt == STB_F32) {
 #pragma unroll
-      for (int k = 0; k < kPiece; ++k) {
-        const int e = pl.at(p, k);
-        if (e >= pl.m) continue;
-        if (dt == STB_F32) static_cast<float*>(row)[e] = v[p][k];
-        else static_cast<unsigned short*>(row)[e] = to_sixteen(v[p][k], dt);
+        for (int k = 0; k < kPiece; ++k)
+          if (pl.at(p, k) < pl.m) static_cast<float*>(row)[pl.at(p, k)] = v[p][k];
+      } else {
+#pragma unroll
+        for (int k = 0; k < kPiece; k += 2) {
+          const uint32_t two = pack_two(v[p][k], v[p][k + 1], dt);
+          if (pl.at(p, k) < pl.m) static_cast<unsigned short*>(row)[pl.at(p, k)] = (unsigned short)two;
+          if (pl.at(p, k + 1) < pl.m) static_cast<unsigned short*>(row)[pl.at(p, k + 1)] = (unsigned short)(two >> 16);
+        }
       }
     }
   }
 }
 
+// ---- pieces on their way -----------------------------------------------------------------------------------------------------------
+// A row's pieces of a thread in shared memory: 16-byte part j of piece p at (parts p + j) width + lane, parts = 1 or, fp32, 2.
+__device__ __forceinline__ void copy_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_async_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+template <int P>
+__device__ __forceinline__ void ask_row(const RowPlace<true>& pl, const void* row, int dt, uint32_t slots) {
+  const int parts = dt == STB_F32 ? 2 : 1;
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    const int i = pl.at(p, 0);
+    if (i >= pl.m) break;
+    const char* src = static_cast<const char*>(row) + (size_t)i * (8 * parts / 4);
+    const uint32_t dst = slots + (uint32_t)((parts * p) * pl.width + pl.lane) * 16u;
+    copy_async16(dst, src);
+    if (parts == 2) copy_async16(dst + (uint32_t)pl.width * 16u, src + 16);
+  }
+}
+__device__ __forceinline__ uint4 slot_piece(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ void take_piece(const RowPlace<true>& pl, int p, int dt, uint32_t slots, float (&v)[kPiece]) {
+  const bool in = pl.at(p, 0) < pl.m;
+  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+  if (dt == STB_F32) {
+    const uint32_t at = slots + (uint32_t)(2 * p * pl.width + pl.lane) * 16u;
+    const uint4 a = in ? slot_piece(at) : zero, b = in ? slot_piece(at + (uint32_t)pl.width * 16u) : zero;
+    floats_piece(make_float4(__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w)),
+                 make_float4(__uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z), __uint_as_float(b.w)), v);
+  } else {
+    unpack_piece(in ? slot_piece(slots + (uint32_t)(p * pl.width + pl.lane) * 16u) : zero, dt, v);
+  }
+}
+template <int P>
+__device__ __forceinline__ void take_row(const RowPlace<true>& pl, int dt, uint32_t slots, float (&v)[P][kPiece]) {
+#pragma unroll
+  for (int p = 0; p < P; ++p) take_piece(pl, p, dt, slots, v[p]);
+}
+
 // ---- sums and maxima over the threads of a row ----------------------------------------------------------------------------------------
 // kWarp: the row belongs to this warp.  Else to the CTA: every reduction of a kernel has a `slot` of its own in shared memory, so that one
 // barrier does for each.  All orders are fixed.
-constexpr int kSlots = 5;
-struct RowShared { float part[kSlots][32]; };
 template <bool kWarp>
-__device__ __forceinline__ float row_sum(float v, RowShared& sh, int slot) {
+__device__ __forceinline__ float row_sum(float v, float (*part)[32], int slot) {
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
   if (kWarp) return v;
   const int lane = threadIdx.x & 31;
-  if (lane == 0) sh.part[slot][threadIdx.x >> 5] = v;
+  if (lane == 0) part[slot][threadIdx.x >> 5] = v;
   __syncthreads();
-  v = lane < (int)(blockDim.x >> 5) ? sh.part[slot][lane] : 0.0f;
+  v = lane < (int)(blockDim.x >> 5) ? part[slot][lane] : 0.0f;
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
   return v;
 }
 // of the magnitudes' bit patterns: an infinity is above every number and a NaN above that
 template <bool kWarp>
-__device__ __forceinline__ uint32_t row_max(uint32_t v, RowShared& sh, int slot) {
+__device__ __forceinline__ uint32_t row_max(uint32_t v, float (*part)[32], int slot) {
   v = __reduce_max_sync(0xFFFFFFFFu, v);
   if (kWarp) return v;
   const int lane = threadIdx.x & 31;
-  if (lane == 0) sh.part[slot][threadIdx.x >> 5] = __uint_as_float(v);
+  if (lane == 0) part[slot][threadIdx.x >> 5] = __uint_as_float(v);
   __syncthreads();
-  v = lane < (int)(blockDim.x >> 5) ? __float_as_uint(sh.part[slot][lane]) : 0u;
+  v = lane < (int)(blockDim.x >> 5) ? __float_as_uint(part[slot][lane]) : 0u;
   return __reduce_max_sync(0xFFFFFFFFu, v);
 }
 template <int P>
@@ -159,66 +228,87 @@ __device__ __forceinline__ RowScale row_scale(uint32_t bits) {
   s.inverse = live ? __fdiv_rn(127.0f, s.largest) : 0.0f;
   return s;
 }
-// The exact decision between two neighbours where v inverse lies next to the border between them.
-__device__ __noinline__ float border_i8(float v, float t, float largest) {
-  const float k = floorf(fabsf(t));
-  const double a = 254.0 * (double)fabsf(v), c = (2.0 * (double)k + 1.0) * (double)largest;      // both exact
-  const float r = a > c ? k + 1.0f : (a < c ? k : 2.0f * rintf(0.5f * (k + 0.25f)));              // the even one of k, k + 1 on the border itself
-  return copysignf(r, v);
+// The whole number nearest to 127 v / largest, decided between two neighbours by exact products where v inverse lies next to the border between them.
+__device__ __forceinline__ uint32_t value_i8_exact(float v, float inverse, float largest) {
+  const float t = v * inverse;
+  float r = rintf(t);
+  if (fabsf(t - r) > 0.4999f) {
+    const float k = floorf(fabsf(t));
+    const double a = 254.0 * (double)fabsf(v), c = (2.0 * (double)k + 1.0) * (double)largest;      // both exact
+    r = copysignf(a > c ? k + 1.0f : (a < c ? k : 2.0f * rintf(0.5f * (k + 0.25f))), v);           // the even one of k, k + 1 on the border itself
+  }
+  return (uint32_t)(int)r & 0xFFu;
+}
+__device__ __noinline__ uint2 piece_i8_exact(float4 a, float4 b, float inverse, float largest) {
+  const float v[kPiece] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  uint2 q = make_uint2(0u, 0u);
+#pragma unroll
+  for (int k = 0; k < kPiece; ++k) (k < 4 ? q.x : q.y) |= value_i8_exact(v[k], inverse, largest) << (8 * (k & 3));
+  return q;
 }
 constexpr float kRoundBias = 12582912.0f;           // 1.5 * 2^23: adding it rounds to the nearest whole number, whose low byte is the sum's
-// q of one value, in the low byte
-__device__ __forceinline__ uint32_t value_i8(float v, const RowScale& s) {
-  const float t = v * s.inverse;
-  float u = t + kRoundBias;
-  if (fabsf(t - (u - kRoundBias)) > 0.4999f) u = border_i8(v, t, s.largest) + kRoundBias;
-  return __float_as_uint(u);
+// `again(spread)`: told how far one step of a 16-bit value can be from a border all the same, says whether v was changed.
+template <bool kVec, class F>
+__device__ __forceinline__ void store_piece_i8(const RowPlace<kVec>& pl, int8_t* row, int p, float (&v)[kPiece], const RowScale& s, float step, F again) {
+  uint32_t q[kPiece];
+  float off, near;                                  // the farthest from a whole number: 0.5 is a border; the same with one `step` (relative) of the value on top
+  auto round = [&]() {
+    off = near = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kPiece; ++k) {
+      const float u = fmaf(v[k], s.inverse, kRoundBias), r = u - kRoundBias, d = fabsf(fmaf(v[k], s.inverse, -r));
+      off = fmaxf(off, d);
+      if (step > 0.0f) near = fmaxf(near, fmaf(fabsf(r) + 0.5f, step, d));
+      q[k] = __float_as_uint(u);
+    }
+  };
+  round();
+  if (step > 0.0f && again(near)) round();
+  uint2 two = make_uint2(__byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410),
+                         __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410));
+  if (off > 0.4999f) two = piece_i8_exact(make_float4(v[0], v[1], v[2], v[3]), make_float4(v[4], v[5], v[6], v[7]), s.inverse, s.largest);
+  if (s.inverse == 0.0f) two = make_uint2(0u, 0u);  // (infinities and NaN among the values)
+  if (kVec) {
+    *reinterpret_cast<uint2*>(row + pl.at(p, 0)) = two;
+  } else {
+#pragma unroll
+    for (int k = 0; k < kPiece; ++k)
+      if (pl.at(p, k) < pl.m) row[pl.at(p, k)] = (int8_t)(((k < 4 ? two.x : two.y) >> (8 * (k & 3))) & 0xFFu);
+  }
 }
 template <int P, bool kVec>
-__device__ __forceinline__ void store_row_i8(const RowPlace<kVec>& pl, int8_t* row, const float (&v)[P][kPiece], const RowScale& s) {
+__device__ __forceinline__ void store_row_i8(const RowPlace<kVec>& pl, int8_t* row, float (&v)[P][kPiece], const RowScale& s) {
 #pragma unroll
   for (int p = 0; p < P; ++p) {
-    const int i = pl.at(p, 0);
-    if (i >= pl.m) break;
-    uint32_t q[kPiece];
-#pragma unroll
-    for (int k = 0; k < kPiece; ++k) q[k] = s.inverse == 0.0f ? 0u : value_i8(v[p][k], s);
-    if (kVec && i + kPiece <= pl.m) {
-      const uint32_t lo = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
-      const uint32_t hi = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
-      *reinterpret_cast<uint2*>(row + i) = make_uint2(lo, hi);
-    } else {
-#pragma unroll
-      for (int k = 0; k < kPiece; ++k)
-        if (pl.at(p, k) < pl.m) row[pl.at(p, k)] = (int8_t)(q[k] & 0xFFu);
-    }
+    if (pl.at(p, 0) >= pl.m) break;
+    store_piece_i8<kVec>(pl, row, p, v[p], s, 0.0f, [](float) { return false; });
   }
 }
 
 // ---- the gated activation ---------------------------------------------------------------------------------------------------------
-// silu(a) b rounded to fp32 and then to the 16-bit type, as exact arithmetic would: evaluated in fp32 within 2^-21 (expf one unit in the
-// last place, __fdividef two, the sum and the product half a one each), and where both ends of a band of 1.5 times that do not round to
-// the same 16-bit value, in float64.  Products too small for a relative bound in fp32 go that way as well.
-__device__ __noinline__ float gated_exact(float a, float b) {
-  const double d = (double)a;
-  return (float)(d / (1.0 + exp(-d)) * (double)b);
+// silu(a) b rounded to fp32 and then to the 16-bit type, as exact arithmetic would.  In fp32 it is known within (5 + 1.2 |min(a, 0)|) 2^-23 (CUDA's bounds in
+// units in the last place: __expf 2 + 1.173 |a|, of which e / (1 + e) reaches the result, __fdividef 2; the sum and the product half a one each;
+// a >= -80, where nothing leaves fp32's range): both ends of a band somewhat wider are rounded, and nearly always give the same 16-bit value.  Where they
+// do not, that of the smaller magnitude is kept, the other is the next one up, and the pair is marked: it is evaluated in float64 only where the
+// choice would show, in the row's largest magnitude or in the value's 8 bits.
+__device__ __noinline__ uint32_t gated_exact(float a0, float a1, float b0, float b1, int dt) {
+  const double d0 = (double)a0, d1 = (double)a1;
+  return pack_two((float)(d0 / (1.0 + exp(-d0)) * (double)b0), (float)(d1 / (1.0 + exp(-d1)) * (double)b1), dt);
 }
-__device__ __forceinline__ void gated_two(float& a0, float& a1, float b0, float b1, int dt) {
-  constexpr float kBand = 1.5f / 2097152.0f;
-  const float h0 = __fdividef(a0, 1.0f + expf(-a0)) * b0, h1 = __fdividef(a1, 1.0f + expf(-a1)) * b1;
-  const uint32_t lo = pack_two(h0 * (1.0f - kBand), h1 * (1.0f - kBand), dt), hi = pack_two(h0 * (1.0f + kBand), h1 * (1.0f + kBand), dt);
-  constexpr float kTiny = 7.8886091e-31f;           // 2^-100
-  const bool tiny0 = fabsf(h0) < kTiny && a0 != 0.0f && b0 != 0.0f, tiny1 = fabsf(h1) < kTiny && a1 != 0.0f && b1 != 0.0f;
-  uint32_t w = lo;
-  if (lo != hi || tiny0 || tiny1) w = pack_two(gated_exact(a0, b0), gated_exact(a1, b1), dt);
-  unpack_two(w, dt, a0, a1);
+constexpr float kUlp = 1.1920929e-7f;               // 2^-23
+__device__ __forceinline__ void gated_two(float a0, float a1, float b0, float b1, int dt, uint32_t& lo, uint32_t& hi) {
+  const float h0 = __fdividef(a0, 1.0f + __expf(-a0)) * b0, h1 = __fdividef(a1, 1.0f + __expf(-a1)) * b1;
+  const float band0 = fmaf(fminf(a0, 0.0f), -1.5f * kUlp, 6.5f * kUlp), band1 = fmaf(fminf(a1, 0.0f), -1.5f * kUlp, 6.5f * kUlp);
+  lo = pack_two(fmaf(-h0, band0, h0), fmaf(-h1, band1, h1), dt);
+  hi = pack_two(fmaf(h0, band0, h0), fmaf(h1, band1, h1), dt);
 }
-template <int P>
-__device__ __forceinline__ void gated_row(float (&a)[P][kPiece], const float (&b)[P][kPiece], int dt) {
-#pragma unroll
-  for (int p = 0; p < P; ++p)
-#pragma unroll
-    for (int k = 0; k < kPiece; k += 2) gated_two(a[p][k], a[p][k + 1], b[p][k], b[p][k + 1], dt);
+__device__ __forceinline__ uint32_t max_sixteen(uint32_t a, uint32_t b) { return __vmaxu2(a, b & 0x7FFF7FFFu); }
+// the larger half of a pair of magnitudes, as fp32 bits
+__device__ __forceinline__ uint32_t magnitude_bits(uint32_t two, int dt) {
+  const uint32_t one = max(two >> 16, two & 0xFFFFu);
+  float a, b;
+  unpack_two(one, dt, a, b);
+  return __float_as_uint(a);
 }
 
 // ---- stb_quantize_i8 ----------------------------------------------------------------------------------------------------------------
@@ -229,49 +319,236 @@ struct QuantI8Args {
   int8_t* q;
   float* scale;
 };
-// kLong: the row does not fit the registers of a CTA; it is read twice.
-template <int P, bool kVec, bool kWarp, bool kGated, bool kLong>
-__global__ void __launch_bounds__(kMaxRowThreads)
+enum QuantIn { kInWide = 0, kInSixteen = 1, kInGated = 2 };      // fp32; 16 bits; 16 bits, gated
+
+// What a thread holds of a row between its largest magnitude and its 8 bits.
+template <int P, int kIn> struct QuantRow { uint32_t h[P][kPiece / 2]; uint32_t marks; };
+template <int P> struct QuantRow<P, kInWide> { float v[P][kPiece]; };
+
+// Gated pairs: h is the candidate of smaller magnitude, bit 4 p + k of marks says that pair k of piece p has two.
+template <int P>
+__device__ __forceinline__ void gate_piece(QuantRow<P, kInGated>& r, int p, const float (&a)[kPiece], const float (&b)[kPiece], int dt, uint32_t& top_lo, uint32_t& top_hi) {
+  float least = a[0];
+#pragma unroll
+  for (int k = 1; k < kPiece; ++k) least = fminf(least, a[k]);
+#pragma unroll
+  for (int k = 0; k < kPiece / 2; ++k) {
+    uint32_t lo, hi;
+    if (least < -80.0f) lo = hi = gated_exact(a[2 * k], a[2 * k + 1], b[2 * k], b[2 * k + 1], dt);
+    else gated_two(a[2 * k], a[2 * k + 1], b[2 * k], b[2 * k + 1], dt, lo, hi);
+    r.h[p][k] = lo;
+    if (lo != hi) r.marks |= 1u << (4 * p + k);
+    top_lo = max_sixteen(top_lo, lo);
+    top_hi = max_sixteen(top_hi, hi);
+  }
+}
+// Settles the marked pairs of a piece: in float64, from the inputs again, where the 8 bits depend on which of the two candidates it is (a magnitude's next
+// one up: its bits plus one), or, inverse < 0, all of them.  The values lie at `at`, each `step` behind the one before it.
+__device__ __noinline__ uint4 settle_piece(uint4 h, uint32_t marks, const void* xr, const void* xr2, int at, int step, int m, int dt, float inverse, float largest) {
+#pragma unroll
+  for (int k = 0; k < kPiece / 2; ++k) {
+    uint32_t& two = k == 0 ? h.x : (k == 1 ? h.y : (k == 2 ? h.z : h.w));
+    if (!((marks >> k) & 1u)) continue;
+    bool shows = inverse < 0.0f;
+    if (!shows) {
+      float a, b, c, d;
+      unpack_two(two, dt, a, b);
+      unpack_two(two + 0x00010001u, dt, c, d);
+      shows = value_i8_exact(a, inverse, largest) != value_i8_exact(c, inverse, largest) || value_i8_exact(b, inverse, largest) != value_i8_exact(d, inverse, largest);
+    }
+    const int i = at + 2 * k * step, j = i + step;
+    if (shows) {
+      const float a0 = i < m ? load_one(xr, (size_t)i, dt) : 0.0f, b0 = i < m ? load_one(xr2, (size_t)i, dt) : 0.0f;
+      const float a1 = j < m ? load_one(xr, (size_t)j, dt) : 0.0f, b1 = j < m ? load_one(xr2, (size_t)j, dt) : 0.0f;
+      two = gated_exact(a0, a1, b0, b1, dt);
+    }
+  }
+  return h;
+}
+
+// kWarp: a row belongs to a warp, else to the CTA, which takes every gridDim-th one.  kAsync: the pieces of the next row are on their way.
+template <int P, int kIn, bool kVec, bool kWarp, bool kAsync>
+__global__ void __launch_bounds__(kWarp ? 256 : (kAsync ? 512 : kMaxRowThreads), kWarp || (kAsync && (P <= 4 || kIn != kInWide)) ? 2 : 1)
 quantize_i8_kernel(const QuantI8Args args) {
-  __shared__ RowShared sh;
+  extern __shared__ __align__(16) uint8_t slots[];
+  __shared__ float sh[6][32];                       // the parts of a row's three reductions, and of the next one's
   const void *x = args.x, *x2 = args.x2;
   begin_after(x, x2);
-  const int row = kWarp ? (int)(blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5)) : (int)blockIdx.x;
-  if (kWarp && row >= args.rows) return;
-  const int bytes = dtype_bytes(args.dt);
-  const char *xr = static_cast<const char*>(x) + (size_t)row * args.ldx * (size_t)bytes, *xr2 = static_cast<const char*>(x2) + (size_t)row * args.ldx2 * (size_t)bytes;
-  int8_t* qr = args.q + (size_t)row * args.ldq;
-  RowPlace<kVec> pl{kWarp ? (int)(threadIdx.x & 31) : (int)threadIdx.x, kWarp ? 32 : (int)blockDim.x, args.m};
-  const int span = pl.width * kPiece * P;
-  auto read = [&](int base, float (&v)[P][kPiece]) {
-    pl.m = args.m - base;
-    load_row<P, kVec>(pl, xr + (size_t)base * bytes, args.dt, v);
-    if (kGated) {
-      float b[P][kPiece];
-      load_row<P, kVec>(pl, xr2 + (size_t)base * bytes, args.dt, b);
-      gated_row<P>(v, b, args.dt);
+  const int dt = args.dt, bytes = dtype_bytes(dt);
+  const int stride = kWarp ? (int)(gridDim.x * (blockDim.x >> 5)) : (int)gridDim.x;
+  int row = kWarp ? (int)(blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5)) : (int)blockIdx.x, slot = 0;
+  const RowPlace<kVec> pl{kWarp ? (int)(threadIdx.x & 31) : (int)threadIdx.x, kWarp ? 32 : (int)blockDim.x, args.m};
+  const uint32_t slot_x = kAsync ? smem_u32(slots) : 0u, slot_x2 = slot_x + (uint32_t)(P * pl.width) * 16u * (kIn == kInWide ? 2u : 1u);
+  auto row_x = [&](int r) { return static_cast<const char*>(x) + (size_t)r * args.ldx * (size_t)bytes; };
+  auto row_x2 = [&](int r) { return static_cast<const char*>(x2) + (size_t)r * args.ldx2 * (size_t)bytes; };
+  auto ask = [&](int r) {
+    if constexpr (kAsync) {
+      ask_row<P>(pl, row_x(r), dt, slot_x);
+      if (kIn == kInGated) ask_row<P>(pl, row_x2(r), dt, slot_x2);
     }
   };
-  float v[P][kPiece];
-  uint32_t bits = 0;
-  if (kLong) {
-    for (int base = 0; base < args.m; base += span) { read(base, v); bits = max(bits, max_bits<P>(v)); }
-  } else {
-    read(0, v);
-    bits = max_bits<P>(v);
+  auto settle = [&](QuantRow<P, kIn>& r, int p, float inverse, float largest) {
+    if constexpr (kIn == kInGated) {
+      const uint4 h = settle_piece(make_uint4(r.h[p][0], r.h[p][1], r.h[p][2], r.h[p][3]), r.marks >> (4 * p), row_x(row), row_x2(row), pl.at(p, 0), pl.at(0, 1) - pl.at(0, 0), args.m, dt,
+                                   inverse, largest);
+      r.h[p][0] = h.x; r.h[p][1] = h.y; r.h[p][2] = h.z; r.h[p][3] = h.w;
+    }
+  };
+  if (kAsync && row < args.rows) ask(row);
+  for (; row < args.rows; row += stride, slot = 3 - slot) {
+    QuantRow<P, kIn> r;
+    uint32_t bits;
+    if constexpr (kAsync) copy_async_done();
+    if constexpr (kIn == kInWide) {
+      if constexpr (kAsync) take_row<P>(pl, dt, slot_x, r.v);
+      else load_row<P, kVec>(pl, row_x(row), dt, r.v);
+      bits = row_max<kWarp>(max_bits<P>(r.v), sh, slot);
+    } else {
+      uint32_t top_lo = 0, top_hi = 0;
+      r.marks = 0;
+      if constexpr (kIn == kInSixteen && kVec) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+          const int i = pl.at(p, 0);
+          uint4 a = make_uint4(0u, 0u, 0u, 0u);
+          if (i < pl.m) {
+            if constexpr (kAsync) a = slot_piece(slot_x + (uint32_t)(p * pl.width + pl.lane) * 16u);
+            else a = *reinterpret_cast<const uint4*>(row_x(row) + (size_t)i * 2);
+          }
+          r.h[p][0] = a.x; r.h[p][1] = a.y; r.h[p][2] = a.z; r.h[p][3] = a.w;
+        }
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+          for (int k = 0; k < kPiece / 2; ++k) top_lo = max_sixteen(top_lo, r.h[p][k]);
+      } else if constexpr (kIn == kInSixteen) {
+        float v[P][kPiece];
+        load_row<P, kVec>(pl, row_x(row), dt, v);
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+          for (int k = 0; k < kPiece / 2; ++k) {
+            r.h[p][k] = pack_two(v[p][2 * k], v[p][2 * k + 1], dt);
+            top_lo = max_sixteen(top_lo, r.h[p][k]);
+          }
+      } else if constexpr (kAsync) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+          const bool in = pl.at(p, 0) < pl.m;
+          const uint32_t at = (uint32_t)(p * pl.width + pl.lane) * 16u;
+          float a[kPiece], b[kPiece];
+          unpack_piece(in ? slot_piece(slot_x + at) : make_uint4(0u, 0u, 0u, 0u), dt, a);
+          unpack_piece(in ? slot_piece(slot_x2 + at) : make_uint4(0u, 0u, 0u, 0u), dt, b);
+          gate_piece<P>(r, p, a, b, dt, top_lo, top_hi);
+        }
+      } else if constexpr (kVec) {
+        uint4 ra[P], rb[P];
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+          const size_t i = (size_t)pl.at(p, 0) * 2;
+          ra[p] = rb[p] = make_uint4(0u, 0u, 0u, 0u);
+          if (pl.at(p, 0) < pl.m) { ra[p] = *reinterpret_cast<const uint4*>(row_x(row) + i); rb[p] = *reinterpret_cast<const uint4*>(row_x2(row) + i); }
+        }
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+          float a[kPiece], b[kPiece];
+          unpack_piece(ra[p], dt, a);
+          unpack_piece(rb[p], dt, b);
+          gate_piece<P>(r, p, a, b, dt, top_lo, top_hi);
+        }
+      } else {
+        float a[P][kPiece], b[P][kPiece];
+        load_row<P, kVec>(pl, row_x(row), dt, a);
+        load_row<P, kVec>(pl, row_x2(row), dt, b);
+#pragma unroll
+        for (int p = 0; p < P; ++p) gate_piece<P>(r, p, a[p], b[p], dt, top_lo, top_hi);
+      }
+      bits = row_max<kWarp>(magnitude_bits(top_lo, dt), sh, slot);
+      if constexpr (kIn == kInGated) {
+        if (row_max<kWarp>(magnitude_bits(top_hi, dt), sh, slot + 1) != bits) {       // the same for every thread of the row
+          top_lo = 0;
+#pragma unroll
+          for (int p = 0; p < P; ++p) {
+            if ((r.marks >> (4 * p)) & 15u) settle(r, p, -1.0f, 0.0f);
+#pragma unroll
+            for (int k = 0; k < kPiece / 2; ++k) top_lo = max_sixteen(top_lo, r.h[p][k]);
+          }
+          r.marks = 0;
+          bits = row_max<kWarp>(magnitude_bits(top_lo, dt), sh, slot + 2);
+        }
+      }
+    }
+    if (kAsync && row + stride < args.rows) ask(row + stride);        // (this row's pieces have been read: its largest magnitude is known)
+    const RowScale s = row_scale(bits);
+    int8_t* qr = args.q + (size_t)row * args.ldq;
+    if (pl.lane == 0) args.scale[row] = s.scale;
+    if constexpr (kIn == kInWide) {
+      store_row_i8<P, kVec>(pl, qr, r.v, s);
+    } else {
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        if (pl.at(p, 0) >= pl.m) break;
+        float v[kPiece];
+        auto unpack = [&]() {
+#pragma unroll
+          for (int k = 0; k < kPiece / 2; ++k) unpack_two(r.h[p][k], dt, v[2 * k], v[2 * k + 1]);
+        };
+        unpack();
+        if constexpr (kIn == kInGated) {
+          // a step of the 16-bit type is at most 2^-10 (fp16) or 2^-7 of its value, and 2^-24 (fp16) where that is less
+          store_piece_i8<kVec>(pl, qr, p, v, s, dt == STB_F16 ? 9.765625e-4f : 7.8125e-3f, [&](float near) {
+            if (!((r.marks >> (4 * p)) & 15u) || near < 0.4998f - 6.0e-8f * s.inverse) return false;
+            settle(r, p, s.inverse, s.largest);
+            unpack();
+            return true;
+          });
+        } else {
+          store_piece_i8<kVec>(pl, qr, p, v, s, 0.0f, [](float) { return false; });
+        }
+      }
+    }
   }
-  const RowScale s = row_scale(row_max<kWarp>(bits, sh, 0));
-  if (pl.lane == 0) args.scale[row] = s.scale;
-  if (kLong) {
-    for (int base = 0; base < args.m; base += span) { read(base, v); store_row_i8<P, kVec>(pl, qr + base, v, s); }
-  } else {
-    store_row_i8<P, kVec>(pl, qr, v, s);
+}
+// A row that does not fit the registers of a CTA is read twice.
+template <bool kVec, bool kGated>
+__global__ void __launch_bounds__(kMaxRowThreads)
+quantize_i8_long_kernel(const QuantI8Args args) {
+  __shared__ float sh[1][32];
+  const void *x = args.x, *x2 = args.x2;
+  begin_after(x, x2);
+  const int dt = args.dt, bytes = dtype_bytes(dt), row = (int)blockIdx.x, span = kMaxRowThreads * kPiece;
+  const char *xr = static_cast<const char*>(x) + (size_t)row * args.ldx * (size_t)bytes, *xr2 = static_cast<const char*>(x2) + (size_t)row * args.ldx2 * (size_t)bytes;
+  RowPlace<kVec> pl{(int)threadIdx.x, kMaxRowThreads, args.m};
+  float v[1][kPiece];
+  auto read = [&](int base) {
+    pl.m = args.m - base;
+    load_row<1, kVec>(pl, xr + (size_t)base * bytes, dt, v);
+    if (kGated) {
+      float b[1][kPiece];
+      load_row<1, kVec>(pl, xr2 + (size_t)base * bytes, dt, b);
+#pragma unroll
+      for (int k = 0; k < kPiece; k += 2) {
+        uint32_t lo, hi;
+        gated_two(v[0][k], v[0][k + 1], b[0][k], b[0][k + 1], dt, lo, hi);
+        if (lo != hi || fminf(v[0][k], v[0][k + 1]) < -80.0f) lo = gated_exact(v[0][k], v[0][k + 1], b[0][k], b[0][k + 1], dt);
+        unpack_two(lo, dt, v[0][k], v[0][k + 1]);
+      }
+    }
+  };
+  uint32_t bits = 0;
+  for (int base = 0; base < args.m; base += span) { read(base); bits = max(bits, max_bits<1>(v)); if (args.m - base <= span) break; }
+  const RowScale s = row_scale(row_max<false>(bits, sh, 0));
+  if (threadIdx.x == 0) args.scale[row] = s.scale;
+  for (int base = 0; base < args.m; base += span) {
+    read(base);
+    store_row_i8<1, kVec>(pl, args.q + (size_t)row * args.ldq + base, v, s);
+    if (args.m - base <= span) break;
   }
 }
 
 // ---- stb_block_norm -----------------------------------------------------------------------------------------------------------------
 template <int P, bool kVec, bool kWarp>
-__device__ __forceinline__ void norm_row(const RowPlace<kVec>& pl, float (&v)[P][kPiece], int kind, float eps, RowShared& sh, int slot) {
+__device__ __forceinline__ void norm_row(const RowPlace<kVec>& pl, float (&v)[P][kPiece], int kind, float eps, float (*sh)[32], int slot) {
   const float per = __fdiv_rn(1.0f, (float)pl.m);
   if (kind == STB_NORM_LAYER) {
     float sum = 0.0f;
@@ -296,79 +573,138 @@ __device__ __forceinline__ void norm_row(const RowPlace<kVec>& pl, float (&v)[P]
 #pragma unroll
     for (int k = 0; k < kPiece; ++k) v[p][k] *= inv;
 }
-template <int P, bool kVec>
-__device__ __forceinline__ void times_row(const RowPlace<kVec>& pl, float (&v)[P][kPiece], const void* w, int dt) {
-  float f[P][kPiece];
-  load_row<P, kVec>(pl, w, dt, f);
+// v = f(v, the row at w), piece by piece
+template <int P, bool kVec, class F>
+__device__ __forceinline__ void with_row(const RowPlace<kVec>& pl, float (&v)[P][kPiece], const void* w, int dt, F f) {
+  auto piece = [&](int p, int type) {
+    RowPlace<kVec> one = pl;
+    float u[1][kPiece];
+    if (kVec) one.lane += p * pl.width;
+    else one.lane += p * kPiece * pl.width;
+    load_row<1, kVec>(one, w, type, u);
 #pragma unroll
-  for (int p = 0; p < P; ++p)
+    for (int k = 0; k < kPiece; ++k) v[p][k] = f(v[p][k], u[0][k]);
+  };
+  if (dt == STB_F32) {
 #pragma unroll
-    for (int k = 0; k < kPiece; ++k) v[p][k] *= f[p][k];
+    for (int p = 0; p < P; ++p) piece(p, STB_F32);
+  } else {
+#pragma unroll
+    for (int p = 0; p < P; ++p) piece(p, dt);
+  }
 }
-template <int P, bool kVec>
-__device__ __forceinline__ void plus_row(const RowPlace<kVec>& pl, float (&v)[P][kPiece], const void* w, int dt) {
-  float f[P][kPiece];
-  load_row<P, kVec>(pl, w, dt, f);
-#pragma unroll
-  for (int p = 0; p < P; ++p)
-#pragma unroll
-    for (int k = 0; k < kPiece; ++k) v[p][k] += f[p][k];
-}
-template <int P, bool kVec, bool kWarp>
-__global__ void __launch_bounds__(kMaxRowThreads)
-block_norm_kernel(const stb_norm a) {
-  __shared__ RowShared sh;
+template <int P, bool kVec, bool kWarp, bool kAsync>
+__global__ void __launch_bounds__(kWarp ? 256 : (kAsync ? 512 : kMaxRowThreads), kWarp || (kAsync && P <= 4) ? 2 : 1)
+block_norm_kernel(const __grid_constant__ stb_norm a) {
+  extern __shared__ __align__(16) uint8_t slots[];
+  __shared__ float sh[10][32];                      // the parts of a row's five reductions, and of the next one's
   const void *x = a.x, *resid = a.resid, *pw = a.post_weight, *pb = a.post_bias, *gate = a.gate, *w = a.weight, *b = a.bias;
   begin_after(x, resid, pw, pb, gate, w, b);
-  const int row = kWarp ? (int)(blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5)) : (int)blockIdx.x;
-  if (kWarp && row >= a.tokens) return;
+  const int stride = kWarp ? (int)(gridDim.x * (blockDim.x >> 5)) : (int)gridDim.x;
+  int row = kWarp ? (int)(blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5)) : (int)blockIdx.x, slot = 0;
   const RowPlace<kVec> pl{kWarp ? (int)(threadIdx.x & 31) : (int)threadIdx.x, kWarp ? 32 : (int)blockDim.x, a.h};
   auto row_of = [&](const void* base, size_t r, size_t ld, int dt) { return static_cast<const char*>(base) + r * ld * (size_t)dtype_bytes(dt); };
-  float v[P][kPiece], r[P][kPiece];
-  load_row<P, kVec>(pl, row_of(x, row, a.ldx, a.xdt), a.xdt, v);
-  if (resid) load_row<P, kVec>(pl, row_of(resid, row, a.ldr, a.rdt), a.rdt, r);
-  if (a.post) {
-    norm_row<P, kVec, kWarp>(pl, v, a.kind, a.eps, sh, 0);
-    if (pw) times_row<P, kVec>(pl, v, pw, a.wdt);
-    if (pb) plus_row<P, kVec>(pl, v, pb, a.wdt);
-  }
-  if (gate) times_row<P, kVec>(pl, v, row_of(gate, row / a.tokens_per_gate, a.ldgate, a.wdt), a.wdt);
+  const uint32_t slot_x = kAsync ? smem_u32(slots) : 0u, slot_r = slot_x + (uint32_t)(P * pl.width) * 16u * (a.xdt == STB_F32 ? 2u : 1u);
+  auto ask = [&](int r) {
+    if constexpr (kAsync) {
+      ask_row<P>(pl, row_of(x, r, a.ldx, a.xdt), a.xdt, slot_x);
+      if (resid) ask_row<P>(pl, row_of(resid, r, a.ldr, a.rdt), a.rdt, slot_r);
+    }
+  };
+  if (kAsync && row < a.tokens) ask(row);
+  for (; row < a.tokens; row += stride, slot ^= 5) {
+    constexpr bool kEarly = !kAsync && (kWarp || P <= 2);       // the residual's loads beside those of x, where registers hold both
+    float v[P][kPiece], r[kEarly ? P : 1][kPiece];
+    if constexpr (kAsync) {
+      copy_async_done();
+      take_row<P>(pl, a.xdt, slot_x, v);
+    } else {
+      load_row<P, kVec>(pl, row_of(x, row, a.ldx, a.xdt), a.xdt, v);
+      if constexpr (kEarly) {
+        if (resid) load_row<P, kVec>(pl, row_of(resid, row, a.ldr, a.rdt), a.rdt, r);
+      }
+    }
+    auto times = [](float u, float f) { return u * f; };
+    auto plus = [](float u, float f) { return u + f; };
+    if (a.post) {
+      norm_row<P, kVec, kWarp>(pl, v, a.kind, a.eps, sh, slot);
+      if (pw) with_row<P, kVec>(pl, v, pw, a.wdt, times);
+      if (pb) with_row<P, kVec>(pl, v, pb, a.wdt, plus);
+    }
+    if (gate) with_row<P, kVec>(pl, v, row_of(gate, row / a.tokens_per_gate, a.ldgate, a.wdt), a.wdt, times);
+    if (!resid) {
 #pragma unroll
-  for (int p = 0; p < P; ++p)
+      for (int p = 0; p < P; ++p)
 #pragma unroll
-    for (int k = 0; k < kPiece; ++k) v[p][k] = resid ? fmaf(a.alpha, v[p][k], r[p][k]) : a.alpha * v[p][k];
-  if (a.resid_out) store_row<P, kVec>(pl, const_cast<char*>(row_of(a.resid_out, row, a.ldro, a.rdt)), a.rdt, v);
-  if (!a.y && !a.q) return;
-  norm_row<P, kVec, kWarp>(pl, v, a.kind, a.eps, sh, 2);
-  if (w) times_row<P, kVec>(pl, v, w, a.wdt);
-  if (b) plus_row<P, kVec>(pl, v, b, a.wdt);
-  if (a.y) store_row<P, kVec>(pl, const_cast<char*>(row_of(a.y, row, a.ldy, a.ydt)), a.ydt, v);
-  if (a.q) {
-    const RowScale s = row_scale(row_max<kWarp>(max_bits<P>(v), sh, 4));
-    if (pl.lane == 0) a.q_scale[row] = s.scale;
-    store_row_i8<P, kVec>(pl, a.q + (size_t)row * a.ldq, v, s);
+        for (int k = 0; k < kPiece; ++k) v[p][k] *= a.alpha;
+    } else if constexpr (kEarly) {
+#pragma unroll
+      for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int k = 0; k < kPiece; ++k) v[p][k] = fmaf(a.alpha, v[p][k], r[p][k]);
+    } else if constexpr (kAsync) {
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        take_piece(pl, p, a.rdt, slot_r, r[0]);
+#pragma unroll
+        for (int k = 0; k < kPiece; ++k) v[p][k] = fmaf(a.alpha, v[p][k], r[0][k]);
+      }
+    } else {
+      with_row<P, kVec>(pl, v, row_of(resid, row, a.ldr, a.rdt), a.rdt, [&](float u, float f) { return fmaf(a.alpha, u, f); });
+    }
+    if (a.resid_out) store_row<P, kVec>(pl, const_cast<char*>(row_of(a.resid_out, row, a.ldro, a.rdt)), a.rdt, v);
+    const bool more = kAsync && row + stride < a.tokens;
+    if (!a.y && !a.q) {
+      if (more) ask(row + stride);
+      continue;
+    }
+    norm_row<P, kVec, kWarp>(pl, v, a.kind, a.eps, sh, slot + 2);
+    if (more) ask(row + stride);                   // (this row's pieces have been read: its sum is known)
+    if (w) with_row<P, kVec>(pl, v, w, a.wdt, times);
+    if (b) with_row<P, kVec>(pl, v, b, a.wdt, plus);
+    if (a.y) store_row<P, kVec>(pl, const_cast<char*>(row_of(a.y, row, a.ldy, a.ydt)), a.ydt, v);
+    if (a.q) {
+      const RowScale s = row_scale(row_max<kWarp>(max_bits<P>(v), sh, slot + 4));
+      if (pl.lane == 0) a.q_scale[row] = s.scale;
+      store_row_i8<P, kVec>(pl, a.q + (size_t)row * a.ldq, v, s);
+    }
   }
 }
 
-// How rows of `m` values are dealt out.  Few rows: one piece per thread, for the shortest way through a row; many: two, which halves the
-// warps that wait at a barrier.
-struct RowShape { int pieces, threads, rows_per_cta; bool warp, long_row; };
-static RowShape row_shape(int m, int rows) {
-  RowShape s;
-  s.long_row = m > kMaxRow;
-  s.warp = m <= 32 * kPiece * kMaxPieces && (rows > 148 || m <= 32 * kPiece);
-  if (s.warp) {
-    s.pieces = m <= 32 * kPiece ? 1 : (m <= 64 * kPiece ? 2 : 4);
-    s.rows_per_cta = rows >= 148 * 8 ? 8 : (rows >= 148 * 2 ? 2 : 1);
-    s.threads = 32 * s.rows_per_cta;
+// ---- launches -----------------------------------------------------------------------------------------------------------------------
+// How rows of m values are dealt out.
+//   warp:    rows of up to 256 values, or of up to 1024 where there are more than SMs; 1 or 4 pieces per lane
+//   async:   more than 296 rows that can be read in 16-byte pieces: 4 pieces per thread (8 beyond 16384 values), as many CTAs as stay on the GPU
+//   else:    one CTA per row, with one piece per thread as long as 1024 threads reach, for the shortest way through a row
+enum RowForm { kRowWarp, kRowAsync, kRowDirect, kRowLong };
+struct RowShape { RowForm form; int pieces, threads, grid; uint32_t smem; };
+static RowShape row_shape(int m, int rows, bool vec, uint32_t slot_bytes_per_piece, uint32_t static_smem) {
+  RowShape s = {};
+  const int pieces = (m + kPiece - 1) / kPiece;
+  if (m > kMaxRow) { s.form = kRowLong; s.pieces = 1; s.threads = kMaxRowThreads; s.grid = rows; return s; }
+  if (m <= 256 || (m <= 1024 && rows > 148)) {
+    const int per_cta = rows >= 148 * 8 ? 8 : (rows >= 148 * 2 ? 2 : 1);
+    s.form = kRowWarp;
+    s.pieces = pieces <= 32 ? 1 : 4;
+    s.threads = 32 * per_cta;
+    s.grid = (rows + per_cta - 1) / per_cta;
     return s;
   }
-  s.rows_per_cta = 1;
-  const int pieces = (m + kPiece - 1) / kPiece;
-  s.pieces = rows > 148 ? 2 : 1;
-  while (s.pieces < kMaxPieces && pieces > s.pieces * kMaxRowThreads) s.pieces *= 2;
+  if (vec && rows > 296) {
+    s.form = kRowAsync;
+    s.pieces = pieces <= 4 * 512 ? 4 : 8;
+    s.threads = ((pieces + s.pieces - 1) / s.pieces + 31) / 32 * 32;
+    s.smem = (uint32_t)(s.pieces * s.threads) * slot_bytes_per_piece;
+    int resident = 1024 / s.threads, by_smem = (int)(228u * 1024u / (s.smem + 1024u + static_smem));
+    if (resident > by_smem) resident = by_smem;
+    if (resident < 1) resident = 1;
+    s.grid = rows < 148 * resident ? rows : 148 * resident;
+    return s;
+  }
+  s.form = kRowDirect;
+  s.pieces = pieces <= kMaxRowThreads ? 1 : (pieces <= 2 * kMaxRowThreads ? 2 : 4);
   s.threads = ((pieces + s.pieces - 1) / s.pieces + 31) / 32 * 32;
-  if (s.threads > kMaxRowThreads) s.threads = kMaxRowThreads;
+  s.grid = rows;
   return s;
 }
 
@@ -376,19 +712,38 @@ static bool rows_aligned(const void* p, size_t ld, int bytes, size_t to) { retur
 static bool element_aligned(const void* p, int dt) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(dtype_bytes(dt) - 1)) == 0; }
 static bool known_dtype(int dt) { return dt == STB_F16 || dt == STB_BF16 || dt == STB_F32; }
 
-template <bool kGated>
-static cudaError_t launch_quantize(const QuantI8Args& a, const RowShape& s, bool vec, cudaStream_t st) {
-  const dim3 grid((unsigned)((a.rows + s.rows_per_cta - 1) / s.rows_per_cta)), block((unsigned)s.threads);
-  auto go = [&](auto kernel) { return launch_after(kernel, grid, block, 0, st, a); };
-  if (s.long_row) return vec ? go(quantize_i8_kernel<2, true, false, kGated, true>) : go(quantize_i8_kernel<2, false, false, kGated, true>);
-  if (s.warp) {
-    if (s.pieces == 1) return vec ? go(quantize_i8_kernel<1, true, true, kGated, false>) : go(quantize_i8_kernel<1, false, true, kGated, false>);
-    if (s.pieces == 2) return vec ? go(quantize_i8_kernel<2, true, true, kGated, false>) : go(quantize_i8_kernel<2, false, true, kGated, false>);
-    return vec ? go(quantize_i8_kernel<4, true, true, kGated, false>) : go(quantize_i8_kernel<4, false, true, kGated, false>);
+// A kernel with more than 48 KB of shared memory has to be allowed it, on every device.
+template <typename K, typename A>
+static cudaError_t launch_rows(K kernel, const RowShape& s, cudaStream_t st, const A& args) {
+  if (s.smem > 48 * 1024) {
+    static bool done[64] = {};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= 64 || !done[dev]) {
+      e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 228 * 1024 - 4096);
+      if (e != cudaSuccess) return e;
+      if (dev >= 0 && dev < 64) done[dev] = true;
+    }
   }
-  if (s.pieces == 1) return vec ? go(quantize_i8_kernel<1, true, false, kGated, false>) : go(quantize_i8_kernel<1, false, false, kGated, false>);
-  if (s.pieces == 2) return vec ? go(quantize_i8_kernel<2, true, false, kGated, false>) : go(quantize_i8_kernel<2, false, false, kGated, false>);
-  return vec ? go(quantize_i8_kernel<4, true, false, kGated, false>) : go(quantize_i8_kernel<4, false, false, kGated, false>);
+  return launch_after(kernel, dim3((unsigned)s.grid), dim3((unsigned)s.threads), s.smem, st, args);
+}
+
+template <int kIn>
+static cudaError_t launch_quantize(const QuantI8Args& a, const RowShape& s, bool vec, cudaStream_t st) {
+  switch (s.form) {
+    case kRowLong:
+      return vec ? launch_rows(quantize_i8_long_kernel<true, kIn == kInGated>, s, st, a) : launch_rows(quantize_i8_long_kernel<false, kIn == kInGated>, s, st, a);
+    case kRowWarp:
+      if (s.pieces == 1) return vec ? launch_rows(quantize_i8_kernel<1, kIn, true, true, false>, s, st, a) : launch_rows(quantize_i8_kernel<1, kIn, false, true, false>, s, st, a);
+      return vec ? launch_rows(quantize_i8_kernel<4, kIn, true, true, false>, s, st, a) : launch_rows(quantize_i8_kernel<4, kIn, false, true, false>, s, st, a);
+    case kRowAsync:
+      return s.pieces == 4 ? launch_rows(quantize_i8_kernel<4, kIn, true, false, true>, s, st, a) : launch_rows(quantize_i8_kernel<8, kIn, true, false, true>, s, st, a);
+    default:
+      if (s.pieces == 1) return vec ? launch_rows(quantize_i8_kernel<1, kIn, true, false, false>, s, st, a) : launch_rows(quantize_i8_kernel<1, kIn, false, false, false>, s, st, a);
+      if (s.pieces == 2) return vec ? launch_rows(quantize_i8_kernel<2, kIn, true, false, false>, s, st, a) : launch_rows(quantize_i8_kernel<2, kIn, false, false, false>, s, st, a);
+      return vec ? launch_rows(quantize_i8_kernel<4, kIn, true, false, false>, s, st, a) : launch_rows(quantize_i8_kernel<4, kIn, false, false, false>, s, st, a);
+  }
 }
 
 }  // namespace stb
@@ -401,12 +756,13 @@ extern "C" int stb_quantize_i8(const void* x, size_t ldx, const void* x2, size_t
   if (ldx < (size_t)m || (x2 && ldx2 < (size_t)m) || ldq < (size_t)m) return STB_ERR_ARG;
   if (!stb::element_aligned(x, xdt) || !stb::element_aligned(x2, xdt) || !stb::element_aligned(scale, STB_F32)) return STB_ERR_ARG;
   const int bytes = stb::dtype_bytes(xdt);
-  const bool vec = stb::rows_aligned(x, ldx, bytes, 16) && stb::rows_aligned(x2, ldx2, bytes, 16) && stb::rows_aligned(q, ldq, 1, 8);
+  const bool vec = m % stb::kPiece == 0 && stb::rows_aligned(x, ldx, bytes, 16) && stb::rows_aligned(x2, ldx2, bytes, 16) && stb::rows_aligned(q, ldq, 1, 8);
   const stb::QuantI8Args a = {x, x2, xdt, rows, m, ldx, ldx2, ldq, q, scale};
-  stb::RowShape s = stb::row_shape(m, rows);
-  if (s.long_row) s.threads = stb::kMaxRowThreads;
+  const stb::RowShape s = stb::row_shape(m, rows, vec, xdt == STB_F32 || x2 ? 32u : 16u, 6u * 128u);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return (x2 ? stb::launch_quantize<true>(a, s, vec, st) : stb::launch_quantize<false>(a, s, vec, st)) == cudaSuccess ? STB_OK : STB_ERR_CUDA;
+  const cudaError_t e = x2 ? stb::launch_quantize<stb::kInGated>(a, s, vec, st)
+                           : (xdt == STB_F32 ? stb::launch_quantize<stb::kInWide>(a, s, vec, st) : stb::launch_quantize<stb::kInSixteen>(a, s, vec, st));
+  return e == cudaSuccess ? STB_OK : STB_ERR_CUDA;
 }
 
 extern "C" int stb_block_norm(const stb_norm* args, void* stream) {
@@ -430,20 +786,23 @@ extern "C" int stb_block_norm(const stb_norm* args, void* stream) {
       !stb::element_aligned(a.gate, a.wdt) || !stb::element_aligned(a.weight, a.wdt) || !stb::element_aligned(a.bias, a.wdt))
     return STB_ERR_ARG;
   const int xb = stb::dtype_bytes(a.xdt), rb = stb::dtype_bytes(a.rdt), wb = stb::dtype_bytes(a.wdt), yb = stb::dtype_bytes(a.ydt);
-  const bool vec = stb::rows_aligned(a.x, a.ldx, xb, 16) && stb::rows_aligned(a.resid, a.ldr, rb, 16) && stb::rows_aligned(a.resid_out, a.ldro, rb, 16) &&
+  const bool vec = a.h % stb::kPiece == 0 && stb::rows_aligned(a.x, a.ldx, xb, 16) && stb::rows_aligned(a.resid, a.ldr, rb, 16) && stb::rows_aligned(a.resid_out, a.ldro, rb, 16) &&
                    stb::rows_aligned(a.y, a.ldy, yb, 16) && stb::rows_aligned(a.q, a.ldq, 1, 8) && stb::rows_aligned(a.gate, a.tokens > a.tokens_per_gate ? a.ldgate : 0, wb, 16) &&
                    stb::rows_aligned(a.post_weight, 0, wb, 16) && stb::rows_aligned(a.post_bias, 0, wb, 16) && stb::rows_aligned(a.weight, 0, wb, 16) &&
                    stb::rows_aligned(a.bias, 0, wb, 16);
-  const stb::RowShape s = stb::row_shape(a.h, a.tokens);
-  const dim3 grid((unsigned)((a.tokens + s.rows_per_cta - 1) / s.rows_per_cta)), block((unsigned)s.threads);
+  const uint32_t slot = (a.xdt == STB_F32 ? 32u : 16u) + (!a.resid ? 0u : (a.rdt == STB_F32 ? 32u : 16u));
+  const stb::RowShape s = stb::row_shape(a.h, a.tokens, vec, slot, 10u * 128u);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  auto go = [&](auto kernel) { return stb::launch_after(kernel, grid, block, 0, st, a) == cudaSuccess ? STB_OK : STB_ERR_CUDA; };
-  if (s.warp) {
-    if (s.pieces == 1) return vec ? go(stb::block_norm_kernel<1, true, true>) : go(stb::block_norm_kernel<1, false, true>);
-    if (s.pieces == 2) return vec ? go(stb::block_norm_kernel<2, true, true>) : go(stb::block_norm_kernel<2, false, true>);
-    return vec ? go(stb::block_norm_kernel<4, true, true>) : go(stb::block_norm_kernel<4, false, true>);
+  auto go = [&](auto kernel) { return stb::launch_rows(kernel, s, st, a) == cudaSuccess ? STB_OK : STB_ERR_CUDA; };
+  switch (s.form) {
+    case stb::kRowWarp:
+      if (s.pieces == 1) return vec ? go(stb::block_norm_kernel<1, true, true, false>) : go(stb::block_norm_kernel<1, false, true, false>);
+      return vec ? go(stb::block_norm_kernel<4, true, true, false>) : go(stb::block_norm_kernel<4, false, true, false>);
+    case stb::kRowAsync:
+      return s.pieces == 4 ? go(stb::block_norm_kernel<4, true, false, true>) : go(stb::block_norm_kernel<8, true, false, true>);
+    default:
+      if (s.pieces == 1) return vec ? go(stb::block_norm_kernel<1, true, false, false>) : go(stb::block_norm_kernel<1, false, false, false>);
+      if (s.pieces == 2) return vec ? go(stb::block_norm_kernel<2, true, false, false>) : go(stb::block_norm_kernel<2, false, false, false>);
+      return vec ? go(stb::block_norm_kernel<4, true, false, false>) : go(stb::block_norm_kernel<4, false, false, false>);
   }
-  if (s.pieces == 1) return vec ? go(stb::block_norm_kernel<1, true, false>) : go(stb::block_norm_kernel<1, false, false>);
-  if (s.pieces == 2) return vec ? go(stb::block_norm_kernel<2, true, false>) : go(stb::block_norm_kernel<2, false, false>);
-  return vec ? go(stb::block_norm_kernel<4, true, false>) : go(stb::block_norm_kernel<4, false, false>);
 }
