@@ -22,6 +22,7 @@ namespace stb {
 constexpr int kPiece = 8;                 // values of a thread in a row, side by side
 constexpr int kMaxRowThreads = 1024;
 constexpr int kMaxRow = 32768;            // values of a row that fit the registers of a CTA
+constexpr int kMaxRowSmem = 224 * 1024;      // dynamic shared memory of a CTA
 constexpr float kSmallestMax = 3.0092655e-36f;      // 2^-118: below it 127 / max would overflow; such a row is zeros with scale 0
 
 __host__ __device__ inline int dtype_bytes(int dt) { return dt == STB_F32 ? 4 : 2; }
@@ -34,13 +35,17 @@ struct RowPlace {
   int lane, width, m;
   __device__ __forceinline__ int at(int p, int k) const { return kVec ? (p * width + lane) * kPiece + k : (p * kPiece + k) * width + lane; }
 };
-__device__ __forceinline__ float load_one(const void* p, size_t i, int dt) {
-  if (dt == STB_F32) return static_cast<const float*>(p)[i];
-  const unsigned short u = static_cast<const unsigned short*>(p)[i];
-  return dt == STB_F16 ? __half2float(__ushort_as_half(u)) : __bfloat162float(__ushort_as_bfloat16(u));
+// The element types are arguments of the calls and template arguments of what runs per value: by_type chooses once per row.
+template <int kType> struct TypeOf { static constexpr int value = kType; };
+template <class F>
+__device__ __forceinline__ void by_type(int dt, F f) {
+  if (dt == STB_F32) f(TypeOf<STB_F32>{});
+  else if (dt == STB_F16) f(TypeOf<STB_F16>{});
+  else f(TypeOf<STB_BF16>{});
 }
-__device__ __forceinline__ void unpack_two(uint32_t w, int dt, float& a, float& b) {
-  if (dt == STB_F16) {
+template <int kType>
+__device__ __forceinline__ void unpack_two(uint32_t w, float& a, float& b) {
+  if (kType == STB_F16) {
     const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
     a = f.x; b = f.y;
   } else {
@@ -48,95 +53,131 @@ __device__ __forceinline__ void unpack_two(uint32_t w, int dt, float& a, float& 
     b = __uint_as_float(w & 0xFFFF0000u);
   }
 }
-__device__ __forceinline__ uint32_t pack_two(float a, float b, int dt) {
-  if (dt == STB_F16) {
+template <int kType>
+__device__ __forceinline__ uint32_t pack_two(float a, float b) {
+  if (kType == STB_F16) {
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
   }
   const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-__device__ __forceinline__ void unpack_piece(const uint4& a, int dt, float (&v)[kPiece]) {
-  unpack_two(a.x, dt, v[0], v[1]); unpack_two(a.y, dt, v[2], v[3]);
-  unpack_two(a.z, dt, v[4], v[5]); unpack_two(a.w, dt, v[6], v[7]);
+template <int kType>
+__device__ __forceinline__ float load_sixteen(const void* p, size_t i) {
+  float a, b;
+  unpack_two<kType>(static_cast<const unsigned short*>(p)[i], a, b);
+  return a;
 }
-__device__ __forceinline__ void floats_piece(const float4& a, const float4& b, float (&v)[kPiece]) {
-  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+template <int kType>
+__device__ __forceinline__ void unpack_piece(const uint4& a, float (&v)[kPiece]) {
+  unpack_two<kType>(a.x, v[0], v[1]); unpack_two<kType>(a.y, v[2], v[3]);
+  unpack_two<kType>(a.z, v[4], v[5]); unpack_two<kType>(a.w, v[6], v[7]);
 }
-// v[p][k] = value at(p, k) of the row that starts at `row`, 0 behind its end.
+// Eight values as they lie in memory: 16 bytes, fp32 twice that.
+template <int kType> struct RawPiece { uint4 w[kType == STB_F32 ? 2 : 1]; };
+template <int kType>
+__device__ __forceinline__ void values_of(const RawPiece<kType>& r, float (&v)[kPiece]) {
+  if constexpr (kType == STB_F32) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      v[4 * h] = __uint_as_float(r.w[h].x); v[4 * h + 1] = __uint_as_float(r.w[h].y); v[4 * h + 2] = __uint_as_float(r.w[h].z); v[4 * h + 3] = __uint_as_float(r.w[h].w);
+    }
+  } else {
+    unpack_piece<kType>(r.w[0], v);
+  }
+}
+// Piece p of the row that starts at `row`: zeros behind its end.
+template <int kType, bool kVec>
+__device__ __forceinline__ RawPiece<kType> load_piece(const RowPlace<kVec>& pl, const void* row, int p) {
+  RawPiece<kType> r;
+  constexpr int kParts = kType == STB_F32 ? 2 : 1;
+#pragma unroll
+  for (int h = 0; h < kParts; ++h) r.w[h] = make_uint4(0u, 0u, 0u, 0u);
+  if constexpr (kVec) {
+    const int i = pl.at(p, 0);
+    if (i < pl.m) {
+      const uint4* q = reinterpret_cast<const uint4*>(static_cast<const char*>(row) + (size_t)i * (2 * kParts));
+#pragma unroll
+      for (int h = 0; h < kParts; ++h) r.w[h] = q[h];
+    }
+  } else if constexpr (kType == STB_F32) {
+    uint32_t u[kPiece];
+#pragma unroll
+    for (int k = 0; k < kPiece; ++k) u[k] = pl.at(p, k) < pl.m ? static_cast<const uint32_t*>(row)[pl.at(p, k)] : 0u;
+    r.w[0] = make_uint4(u[0], u[1], u[2], u[3]);
+    r.w[1] = make_uint4(u[4], u[5], u[6], u[7]);
+  } else {
+    uint32_t u[kPiece];
+#pragma unroll
+    for (int k = 0; k < kPiece; ++k) u[k] = pl.at(p, k) < pl.m ? static_cast<const unsigned short*>(row)[pl.at(p, k)] : 0u;
+    r.w[0] = make_uint4(u[0] | (u[1] << 16), u[2] | (u[3] << 16), u[4] | (u[5] << 16), u[6] | (u[7] << 16));
+  }
+  return r;
+}
+// f(p, values) for every piece of the row at `row`, after all of its loads have been asked for.
+template <int P, bool kVec, class F>
+__device__ __forceinline__ void for_row(const RowPlace<kVec>& pl, const void* row, int dt, F f) {
+  by_type(dt, [&](auto type) {
+    constexpr int kType = decltype(type)::value;
+    constexpr int kAtOnce = kType == STB_F32 && P > 2 ? 2 : P;      // (registers)
+#pragma unroll
+    for (int p0 = 0; p0 < P; p0 += kAtOnce) {
+      RawPiece<kType> raw[kAtOnce];
+#pragma unroll
+      for (int p = 0; p < kAtOnce; ++p) raw[p] = load_piece<kType, kVec>(pl, row, p0 + p);
+#pragma unroll
+      for (int p = 0; p < kAtOnce; ++p) {
+        float u[kPiece];
+        values_of<kType>(raw[p], u);
+        f(p0 + p, u);
+      }
+    }
+  });
+}
 template <int P, bool kVec>
 __device__ __forceinline__ void load_row(const RowPlace<kVec>& pl, const void* row, int dt, float (&v)[P][kPiece]) {
-  if (kVec && dt == STB_F32) {
+  by_type(dt, [&](auto type) {
+    constexpr int kType = decltype(type)::value;
+    RawPiece<kType> raw[P];
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
-      const int i = pl.at(p, 0);
-      float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f), b = a;
-      if (i < pl.m) { const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(row) + i); a = q[0]; b = q[1]; }
-      floats_piece(a, b, v[p]);
-    }
-  } else if (kVec) {
-    uint4 a[P];
+    for (int p = 0; p < P; ++p) raw[p] = load_piece<kType, kVec>(pl, row, p);
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
-      const int i = pl.at(p, 0);
-      a[p] = make_uint4(0u, 0u, 0u, 0u);
-      if (i < pl.m) a[p] = *reinterpret_cast<const uint4*>(static_cast<const unsigned short*>(row) + i);
-    }
-#pragma unroll
-    for (int p = 0; p < P; ++p) unpack_piece(a[p], dt, v[p]);
-  } else if (dt == STB_F32) {
-#pragma unroll
-    for (int p = 0; p < P; ++p)
-#pragma unroll
-      for (int k = 0; k < kPiece; ++k) {
-        const int e = pl.at(p, k);
-        v[p][k] = e < pl.m ? static_cast<const float*>(row)[e] : 0.0f;
-      }
-  } else {
-    unsigned short u[P][kPiece];
-#pragma unroll
-    for (int p = 0; p < P; ++p)
-#pragma unroll
-      for (int k = 0; k < kPiece; ++k) {
-        const int e = pl.at(p, k);
-        u[p][k] = e < pl.m ? static_cast<const unsigned short*>(row)[e] : (unsigned short)0;
-      }
-#pragma unroll
-    for (int p = 0; p < P; ++p)
-#pragma unroll
-      for (int k = 0; k < kPiece; k += 2) unpack_two((uint32_t)u[p][k] | ((uint32_t)u[p][k + 1] << 16), dt, v[p][k], v[p][k + 1]);
-  }
+    for (int p = 0; p < P; ++p) values_of<kType>(raw[p], v[p]);
+  });
 }
 template <int P, bool kVec>
 __device__ __forceinline__ void store_row(const RowPlace<kVec>& pl, void* row, int dt, const float (&v)[P][kPiece]) {
+  by_type(dt, [&](auto type) {
+    constexpr int kType = decltype(type)::value;
 #pragma unroll
-  for (int p = 0; p < P; ++p) {
-    const int i = pl.at(p, 0);
-    if (kVec) {
-      if (i >= pl.m) break;
-      if (dt == STB_F32) {
-        float4* q = reinterpret_cast<float4*>(static_cast<float*>(row) + i);
-        q[0] = make_float4(v[p][0], v[p][1], v[p][2], v[p][3]);
-        q[1] = make_float4(v[p][4], v[p][5], v[p][6], v[p][7]);
+    for (int p = 0; p < P; ++p) {
+      const int i = pl.at(p, 0);
+      if (kVec && i >= pl.m) break;
+      if constexpr (kType == STB_F32) {
+        float* q = static_cast<float*>(row);
+        if (kVec) {
+          reinterpret_cast<float4*>(q + i)[0] = make_float4(v[p][0], v[p][1], v[p][2], v[p][3]);
+          reinterpret_cast<float4*>(q + i)[1] = make_float4(v[p][4], v[p][5], v[p][6], v[p][7]);
+        } else {
+#pragma unroll
+          for (int k = 0; k < kPiece; ++k)
+            if (pl.at(p, k) < pl.m) q[pl.at(p, k)] = v[p][k];
+        }
       } else {
-        *reinterpret_cast<uint4*>(static_cast<unsigned short*>(row) + i) =
-            make_uint4(pack_two(v[p][0], v[p][1], dt), pack_two(v[p][2], v[p][3], dt), pack_two(v[p][4], v[p][5], dt), pack_two(v[p][6], v[p][7], dt));
-      }
-    } else {
-      if (dt == STB_F32) {
+        unsigned short* q = static_cast<unsigned short*>(row);
+        uint32_t w[kPiece / 2];
 #pragma unroll
-        for (int k = 0; k < kPiece; ++k)
-          if (pl.at(p, k) < pl.m) static_cast<float*>(row)[pl.at(p, k)] = v[p][k];
-      } else {
+        for (int k = 0; k < kPiece / 2; ++k) w[k] = pack_two<kType>(v[p][2 * k], v[p][2 * k + 1]);
+        if (kVec) {
+          *reinterpret_cast<uint4*>(q + i) = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
 #pragma unroll
-        for (int k = 0; k < kPiece; k += 2) {
-          const uint32_t two = pack_two(v[p][k], v[p][k + 1], dt);
-          if (pl.at(p, k) < pl.m) static_cast<unsigned short*>(row)[pl.at(p, k)] = (unsigned short)two;
-          if (pl.at(p, k + 1) < pl.m) static_cast<unsigned short*>(row)[pl.at(p, k + 1)] = (unsigned short)(two >> 16);
+          for (int k = 0; k < kPiece; ++k)
+            if (pl.at(p, k) < pl.m) q[pl.at(p, k)] = (unsigned short)(w[k >> 1] >> (16 * (k & 1)));
         }
       }
     }
-  }
+  });
 }
 
 // ---- pieces on their way -----------------------------------------------------------------------------------------------------------
@@ -163,22 +204,27 @@ __device__ __forceinline__ uint4 slot_piece(uint32_t a) {
   asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
   return v;
 }
-__device__ __forceinline__ void take_piece(const RowPlace<true>& pl, int p, int dt, uint32_t slots, float (&v)[kPiece]) {
-  const bool in = pl.at(p, 0) < pl.m;
-  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-  if (dt == STB_F32) {
-    const uint32_t at = slots + (uint32_t)(2 * p * pl.width + pl.lane) * 16u;
-    const uint4 a = in ? slot_piece(at) : zero, b = in ? slot_piece(at + (uint32_t)pl.width * 16u) : zero;
-    floats_piece(make_float4(__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w)),
-                 make_float4(__uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z), __uint_as_float(b.w)), v);
-  } else {
-    unpack_piece(in ? slot_piece(slots + (uint32_t)(p * pl.width + pl.lane) * 16u) : zero, dt, v);
-  }
-}
-template <int P>
-__device__ __forceinline__ void take_row(const RowPlace<true>& pl, int dt, uint32_t slots, float (&v)[P][kPiece]) {
+template <int kType>
+__device__ __forceinline__ RawPiece<kType> slot_raw(const RowPlace<true>& pl, int p, uint32_t slots) {
+  constexpr int kParts = kType == STB_F32 ? 2 : 1;
+  RawPiece<kType> r;
 #pragma unroll
-  for (int p = 0; p < P; ++p) take_piece(pl, p, dt, slots, v[p]);
+  for (int h = 0; h < kParts; ++h)
+    r.w[h] = pl.at(p, 0) < pl.m ? slot_piece(slots + (uint32_t)((kParts * p + h) * pl.width + pl.lane) * 16u) : make_uint4(0u, 0u, 0u, 0u);
+  return r;
+}
+// f(p, values) for every piece in the slots
+template <int P, class F>
+__device__ __forceinline__ void for_slots(const RowPlace<true>& pl, int dt, uint32_t slots, F f) {
+  by_type(dt, [&](auto type) {
+    constexpr int kType = decltype(type)::value;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      float u[kPiece];
+      values_of<kType>(slot_raw<kType>(pl, p, slots), u);
+      f(p, u);
+    }
+  });
 }
 
 // ---- sums and maxima over the threads of a row ----------------------------------------------------------------------------------------
@@ -247,23 +293,16 @@ __device__ __noinline__ uint2 piece_i8_exact(float4 a, float4 b, float inverse, 
   return q;
 }
 constexpr float kRoundBias = 12582912.0f;           // 1.5 * 2^23: adding it rounds to the nearest whole number, whose low byte is the sum's
-// `again(spread)`: told how far one step of a 16-bit value can be from a border all the same, says whether v was changed.
-template <bool kVec, class F>
-__device__ __forceinline__ void store_piece_i8(const RowPlace<kVec>& pl, int8_t* row, int p, float (&v)[kPiece], const RowScale& s, float step, F again) {
+template <bool kVec>
+__device__ __forceinline__ void store_piece_i8(const RowPlace<kVec>& pl, int8_t* row, int p, const float (&v)[kPiece], const RowScale& s) {
   uint32_t q[kPiece];
-  float off, near;                                  // the farthest from a whole number: 0.5 is a border; the same with one `step` (relative) of the value on top
-  auto round = [&]() {
-    off = near = 0.0f;
+  float off = 0.0f;                                 // the farthest from a whole number: 0.5 is a border
 #pragma unroll
-    for (int k = 0; k < kPiece; ++k) {
-      const float u = fmaf(v[k], s.inverse, kRoundBias), r = u - kRoundBias, d = fabsf(fmaf(v[k], s.inverse, -r));
-      off = fmaxf(off, d);
-      if (step > 0.0f) near = fmaxf(near, fmaf(fabsf(r) + 0.5f, step, d));
-      q[k] = __float_as_uint(u);
-    }
-  };
-  round();
-  if (step > 0.0f && again(near)) round();
+  for (int k = 0; k < kPiece; ++k) {
+    const float u = fmaf(v[k], s.inverse, kRoundBias);
+    off = fmaxf(off, fabsf(fmaf(v[k], s.inverse, -(u - kRoundBias))));
+    q[k] = __float_as_uint(u);
+  }
   uint2 two = make_uint2(__byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410),
                          __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410));
   if (off > 0.4999f) two = piece_i8_exact(make_float4(v[0], v[1], v[2], v[3]), make_float4(v[4], v[5], v[6], v[7]), s.inverse, s.largest);
@@ -277,74 +316,57 @@ __device__ __forceinline__ void store_piece_i8(const RowPlace<kVec>& pl, int8_t*
   }
 }
 template <int P, bool kVec>
-__device__ __forceinline__ void store_row_i8(const RowPlace<kVec>& pl, int8_t* row, float (&v)[P][kPiece], const RowScale& s) {
+__device__ __forceinline__ void store_row_i8(const RowPlace<kVec>& pl, int8_t* row, const float (&v)[P][kPiece], const RowScale& s) {
 #pragma unroll
   for (int p = 0; p < P; ++p) {
     if (pl.at(p, 0) >= pl.m) break;
-    store_piece_i8<kVec>(pl, row, p, v[p], s, 0.0f, [](float) { return false; });
+    store_piece_i8<kVec>(pl, row, p, v[p], s);
   }
 }
 
 // ---- the gated activation ---------------------------------------------------------------------------------------------------------
-// silu(a) b rounded to fp32 and then to the 16-bit type, as exact arithmetic would.  In fp32 it is known within (5 + 1.2 |min(a, 0)|) 2^-23 (CUDA's bounds in
-// units in the last place: __expf 2 + 1.173 |a|, of which e / (1 + e) reaches the result, __fdividef 2; the sum and the product half a one each;
-// a >= -80, where nothing leaves fp32's range): both ends of a band somewhat wider are rounded, and nearly always give the same 16-bit value.  Where they
+// silu(a) b rounded to fp32 and then to the 16-bit type, as exact arithmetic would.  In fp32 it is known within (5 + 0.75 |min(a, 0)|) 2^-23 (in units of 2^-23: the power
+// of two 2 by its specification and 0.75 |a| from its rounded argument, of which e / (1 + e) reaches the result, the reciprocal 1, the sum, the two products and the
+// fp32 rounding half a one each; a >= -80, where nothing leaves fp32's range): both ends of a band somewhat wider are rounded, and nearly always give the same 16-bit value.  Where they
 // do not, that of the smaller magnitude is kept, the other is the next one up, and the pair is marked: it is evaluated in float64 only where the
 // choice would show, in the row's largest magnitude or in the value's 8 bits.
-__device__ __noinline__ uint32_t gated_exact(float a0, float a1, float b0, float b1, int dt) {
+template <int kType>
+__device__ __noinline__ uint32_t gated_exact(float a0, float a1, float b0, float b1) {
   const double d0 = (double)a0, d1 = (double)a1;
-  return pack_two((float)(d0 / (1.0 + exp(-d0)) * (double)b0), (float)(d1 / (1.0 + exp(-d1)) * (double)b1), dt);
+  return pack_two<kType>((float)(d0 / (1.0 + exp(-d0)) * (double)b0), (float)(d1 / (1.0 + exp(-d1)) * (double)b1));
 }
 constexpr float kUlp = 1.1920929e-7f;               // 2^-23
-__device__ __forceinline__ void gated_two(float a0, float a1, float b0, float b1, int dt, uint32_t& lo, uint32_t& hi) {
-  const float h0 = __fdividef(a0, 1.0f + __expf(-a0)) * b0, h1 = __fdividef(a1, 1.0f + __expf(-a1)) * b1;
-  const float band0 = fmaf(fminf(a0, 0.0f), -1.5f * kUlp, 6.5f * kUlp), band1 = fmaf(fminf(a1, 0.0f), -1.5f * kUlp, 6.5f * kUlp);
-  lo = pack_two(fmaf(-h0, band0, h0), fmaf(-h1, band1, h1), dt);
-  hi = pack_two(fmaf(h0, band0, h0), fmaf(h1, band1, h1), dt);
+__device__ __forceinline__ float gated_one(float a, float b) {
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(a * -1.4426950408889634f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+  return a * r * b;
 }
-__device__ __forceinline__ uint32_t max_sixteen(uint32_t a, uint32_t b) { return __vmaxu2(a, b & 0x7FFF7FFFu); }
-// the larger half of a pair of magnitudes, as fp32 bits
-__device__ __forceinline__ uint32_t magnitude_bits(uint32_t two, int dt) {
-  const uint32_t one = max(two >> 16, two & 0xFFFFu);
-  float a, b;
-  unpack_two(one, dt, a, b);
-  return __float_as_uint(a);
+template <int kType>
+__device__ __forceinline__ void gated_two(float a0, float a1, float b0, float b1, uint32_t& lo, uint32_t& hi) {
+  const float h0 = gated_one(a0, b0), h1 = gated_one(a1, b1);
+  const float band0 = fmaf(fminf(a0, 0.0f), -kUlp, 6.0f * kUlp), band1 = fmaf(fminf(a1, 0.0f), -kUlp, 6.0f * kUlp);
+  lo = pack_two<kType>(fmaf(-h0, band0, h0), fmaf(-h1, band1, h1));
+  hi = pack_two<kType>(fmaf(h0, band0, h0), fmaf(h1, band1, h1));
 }
 
 // ---- stb_quantize_i8 ----------------------------------------------------------------------------------------------------------------
 struct QuantI8Args {
   const void *x, *x2;
-  int dt, rows, m;
+  int rows, m;
   size_t ldx, ldx2, ldq;
   int8_t* q;
   float* scale;
 };
-enum QuantIn { kInWide = 0, kInSixteen = 1, kInGated = 2 };      // fp32; 16 bits; 16 bits, gated
+// The values: of kType as they are, or (16-bit types) gated.  What a thread holds of a row between its largest magnitude and its 8 bits.  Gated pairs: h is
+// the candidate of smaller magnitude, bit 4 p + k of marks says that pair k of piece p has two.
+template <int P, int kType> struct QuantRow { uint32_t h[P][kPiece / 2]; uint32_t marks; };
+template <int P> struct QuantRow<P, STB_F32> { float v[P][kPiece]; uint32_t marks; };
 
-// What a thread holds of a row between its largest magnitude and its 8 bits.
-template <int P, int kIn> struct QuantRow { uint32_t h[P][kPiece / 2]; uint32_t marks; };
-template <int P> struct QuantRow<P, kInWide> { float v[P][kPiece]; };
-
-// Gated pairs: h is the candidate of smaller magnitude, bit 4 p + k of marks says that pair k of piece p has two.
-template <int P>
-__device__ __forceinline__ void gate_piece(QuantRow<P, kInGated>& r, int p, const float (&a)[kPiece], const float (&b)[kPiece], int dt, uint32_t& top_lo, uint32_t& top_hi) {
-  float least = a[0];
-#pragma unroll
-  for (int k = 1; k < kPiece; ++k) least = fminf(least, a[k]);
-#pragma unroll
-  for (int k = 0; k < kPiece / 2; ++k) {
-    uint32_t lo, hi;
-    if (least < -80.0f) lo = hi = gated_exact(a[2 * k], a[2 * k + 1], b[2 * k], b[2 * k + 1], dt);
-    else gated_two(a[2 * k], a[2 * k + 1], b[2 * k], b[2 * k + 1], dt, lo, hi);
-    r.h[p][k] = lo;
-    if (lo != hi) r.marks |= 1u << (4 * p + k);
-    top_lo = max_sixteen(top_lo, lo);
-    top_hi = max_sixteen(top_hi, hi);
-  }
-}
 // Settles the marked pairs of a piece: in float64, from the inputs again, where the 8 bits depend on which of the two candidates it is (a magnitude's next
 // one up: its bits plus one), or, inverse < 0, all of them.  The values lie at `at`, each `step` behind the one before it.
-__device__ __noinline__ uint4 settle_piece(uint4 h, uint32_t marks, const void* xr, const void* xr2, int at, int step, int m, int dt, float inverse, float largest) {
+template <int kType>
+__device__ __noinline__ uint4 settle_piece(uint4 h, uint32_t marks, const void* xr, const void* xr2, int at, int step, int m, float inverse, float largest) {
 #pragma unroll
   for (int k = 0; k < kPiece / 2; ++k) {
     uint32_t& two = k == 0 ? h.x : (k == 1 ? h.y : (k == 2 ? h.z : h.w));
@@ -352,197 +374,192 @@ __device__ __noinline__ uint4 settle_piece(uint4 h, uint32_t marks, const void* 
     bool shows = inverse < 0.0f;
     if (!shows) {
       float a, b, c, d;
-      unpack_two(two, dt, a, b);
-      unpack_two(two + 0x00010001u, dt, c, d);
+      unpack_two<kType>(two, a, b);
+      unpack_two<kType>(two + 0x00010001u, c, d);
       shows = value_i8_exact(a, inverse, largest) != value_i8_exact(c, inverse, largest) || value_i8_exact(b, inverse, largest) != value_i8_exact(d, inverse, largest);
     }
     const int i = at + 2 * k * step, j = i + step;
     if (shows) {
-      const float a0 = i < m ? load_one(xr, (size_t)i, dt) : 0.0f, b0 = i < m ? load_one(xr2, (size_t)i, dt) : 0.0f;
-      const float a1 = j < m ? load_one(xr, (size_t)j, dt) : 0.0f, b1 = j < m ? load_one(xr2, (size_t)j, dt) : 0.0f;
-      two = gated_exact(a0, a1, b0, b1, dt);
+      const float a0 = i < m ? load_sixteen<kType>(xr, (size_t)i) : 0.0f, b0 = i < m ? load_sixteen<kType>(xr2, (size_t)i) : 0.0f;
+      const float a1 = j < m ? load_sixteen<kType>(xr, (size_t)j) : 0.0f, b1 = j < m ? load_sixteen<kType>(xr2, (size_t)j) : 0.0f;
+      two = gated_exact<kType>(a0, a1, b0, b1);
     }
   }
   return h;
 }
-
+// The gated values of a piece.  top: per half the largest of 2 magnitude + (whether there are two candidates), of the larger candidates.
+template <int P, int kType>
+__device__ __forceinline__ void gate_piece(QuantRow<P, kType>& r, int p, const uint4& ra, const uint4& rb, uint32_t& top) {
+  float a[kPiece], b[kPiece];
+  unpack_piece<kType>(ra, a);
+  unpack_piece<kType>(rb, b);
+  float least = a[0];
+#pragma unroll
+  for (int k = 1; k < kPiece; ++k) least = fminf(least, a[k]);
+#pragma unroll
+  for (int k = 0; k < kPiece / 2; ++k) {
+    uint32_t lo, hi;
+    gated_two<kType>(a[2 * k], a[2 * k + 1], b[2 * k], b[2 * k + 1], lo, hi);
+    if (least < -80.0f) lo = hi = gated_exact<kType>(a[2 * k], a[2 * k + 1], b[2 * k], b[2 * k + 1]);
+    r.h[p][k] = lo;
+    const bool two = ((lo ^ hi) & 0x7FFF7FFFu) != 0u;      // (a zero's sign says nothing)
+    if (two) r.marks |= 1u << (4 * p + k);
+    top = __vmaxu2(top, ((hi << 1) & 0xFFFEFFFEu) | (two ? 0x00010001u : 0u));
+  }
+}
+// fp32 bits of a 16-bit magnitude
+template <int kType>
+__device__ __forceinline__ uint32_t magnitude_bits(uint32_t m) {
+  float a, b;
+  unpack_two<kType>(m, a, b);
+  return __float_as_uint(a);
+}
 // kWarp: a row belongs to a warp, else to the CTA, which takes every gridDim-th one.  kAsync: the pieces of the next row are on their way.
-template <int P, int kIn, bool kVec, bool kWarp, bool kAsync>
-__global__ void __launch_bounds__(kWarp ? 256 : (kAsync ? 512 : kMaxRowThreads), kWarp || (kAsync && (P <= 4 || kIn != kInWide)) ? 2 : 1)
+template <int P, int kType, bool kGated, bool kVec, bool kWarp, bool kAsync>
+__global__ void __launch_bounds__(kWarp ? 256 : (kAsync ? 512 : kMaxRowThreads), kWarp || (kAsync && (P <= 4 || kType != STB_F32)) ? 2 : 1)
 quantize_i8_kernel(const QuantI8Args args) {
   extern __shared__ __align__(16) uint8_t slots[];
-  __shared__ float sh[6][32];                       // the parts of a row's three reductions, and of the next one's
+  __shared__ float sh[4][32];                       // the parts of a row's two reductions, and of the next one's
   const void *x = args.x, *x2 = args.x2;
   begin_after(x, x2);
-  const int dt = args.dt, bytes = dtype_bytes(dt);
+  constexpr int kBytes = kType == STB_F32 ? 4 : 2;
   const int stride = kWarp ? (int)(gridDim.x * (blockDim.x >> 5)) : (int)gridDim.x;
   int row = kWarp ? (int)(blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5)) : (int)blockIdx.x, slot = 0;
   const RowPlace<kVec> pl{kWarp ? (int)(threadIdx.x & 31) : (int)threadIdx.x, kWarp ? 32 : (int)blockDim.x, args.m};
-  const uint32_t slot_x = kAsync ? smem_u32(slots) : 0u, slot_x2 = slot_x + (uint32_t)(P * pl.width) * 16u * (kIn == kInWide ? 2u : 1u);
-  auto row_x = [&](int r) { return static_cast<const char*>(x) + (size_t)r * args.ldx * (size_t)bytes; };
-  auto row_x2 = [&](int r) { return static_cast<const char*>(x2) + (size_t)r * args.ldx2 * (size_t)bytes; };
+  const uint32_t slot_x = kAsync ? smem_u32(slots) : 0u, slot_x2 = slot_x + (uint32_t)(P * pl.width) * 16u;
+  auto row_x = [&](int r) { return static_cast<const char*>(x) + (size_t)r * args.ldx * kBytes; };
+  auto row_x2 = [&](int r) { return static_cast<const char*>(x2) + (size_t)r * args.ldx2 * kBytes; };
   auto ask = [&](int r) {
     if constexpr (kAsync) {
-      ask_row<P>(pl, row_x(r), dt, slot_x);
-      if (kIn == kInGated) ask_row<P>(pl, row_x2(r), dt, slot_x2);
+      ask_row<P>(pl, row_x(r), kType, slot_x);
+      if (kGated) ask_row<P>(pl, row_x2(r), kType, slot_x2);
     }
   };
-  auto settle = [&](QuantRow<P, kIn>& r, int p, float inverse, float largest) {
-    if constexpr (kIn == kInGated) {
-      const uint4 h = settle_piece(make_uint4(r.h[p][0], r.h[p][1], r.h[p][2], r.h[p][3]), r.marks >> (4 * p), row_x(row), row_x2(row), pl.at(p, 0), pl.at(0, 1) - pl.at(0, 0), args.m, dt,
-                                   inverse, largest);
+  auto settle = [&](QuantRow<P, kType>& r, int p, float inverse, float largest) {
+    if constexpr (kGated) {
+      const uint4 h = settle_piece<kType>(make_uint4(r.h[p][0], r.h[p][1], r.h[p][2], r.h[p][3]), r.marks >> (4 * p), row_x(row), row_x2(row), pl.at(p, 0), pl.at(0, 1) - pl.at(0, 0), args.m,
+                                          inverse, largest);
       r.h[p][0] = h.x; r.h[p][1] = h.y; r.h[p][2] = h.z; r.h[p][3] = h.w;
     }
   };
   if (kAsync && row < args.rows) ask(row);
-  for (; row < args.rows; row += stride, slot = 3 - slot) {
-    QuantRow<P, kIn> r;
+  for (; row < args.rows; row += stride, slot ^= 2) {
+    QuantRow<P, kType> r;
+    r.marks = 0;
     uint32_t bits;
     if constexpr (kAsync) copy_async_done();
-    if constexpr (kIn == kInWide) {
-      if constexpr (kAsync) take_row<P>(pl, dt, slot_x, r.v);
-      else load_row<P, kVec>(pl, row_x(row), dt, r.v);
+    RawPiece<kType> raw[P], raw2[kGated && !kAsync ? P : 1];
+    if constexpr (!kAsync) {
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        raw[p] = load_piece<kType, kVec>(pl, row_x(row), p);
+        if constexpr (kGated) raw2[p] = load_piece<kType, kVec>(pl, row_x2(row), p);
+      }
+    }
+    if constexpr (kType == STB_F32) {
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        if constexpr (kAsync) raw[p] = slot_raw<kType>(pl, p, slot_x);
+        values_of<kType>(raw[p], r.v[p]);
+      }
       bits = row_max<kWarp>(max_bits<P>(r.v), sh, slot);
     } else {
-      uint32_t top_lo = 0, top_hi = 0;
-      r.marks = 0;
-      if constexpr (kIn == kInSixteen && kVec) {
+      uint32_t top = 0;
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-          const int i = pl.at(p, 0);
-          uint4 a = make_uint4(0u, 0u, 0u, 0u);
-          if (i < pl.m) {
-            if constexpr (kAsync) a = slot_piece(slot_x + (uint32_t)(p * pl.width + pl.lane) * 16u);
-            else a = *reinterpret_cast<const uint4*>(row_x(row) + (size_t)i * 2);
-          }
-          r.h[p][0] = a.x; r.h[p][1] = a.y; r.h[p][2] = a.z; r.h[p][3] = a.w;
+      for (int p = 0; p < P; ++p) {
+        if constexpr (kAsync) raw[p] = slot_raw<kType>(pl, p, slot_x);
+        if constexpr (kGated) {
+          if constexpr (kAsync) raw2[0] = slot_raw<kType>(pl, p, slot_x2);
+          gate_piece<P, kType>(r, p, raw[p].w[0], raw2[kAsync ? 0 : p].w[0], top);
+        } else {
+          r.h[p][0] = raw[p].w[0].x; r.h[p][1] = raw[p].w[0].y; r.h[p][2] = raw[p].w[0].z; r.h[p][3] = raw[p].w[0].w;
+#pragma unroll
+          for (int k = 0; k < kPiece / 2; ++k) top = __vmaxu2(top, r.h[p][k] & 0x7FFF7FFFu);
         }
-#pragma unroll
-        for (int p = 0; p < P; ++p)
-#pragma unroll
-          for (int k = 0; k < kPiece / 2; ++k) top_lo = max_sixteen(top_lo, r.h[p][k]);
-      } else if constexpr (kIn == kInSixteen) {
-        float v[P][kPiece];
-        load_row<P, kVec>(pl, row_x(row), dt, v);
-#pragma unroll
-        for (int p = 0; p < P; ++p)
-#pragma unroll
-          for (int k = 0; k < kPiece / 2; ++k) {
-            r.h[p][k] = pack_two(v[p][2 * k], v[p][2 * k + 1], dt);
-            top_lo = max_sixteen(top_lo, r.h[p][k]);
-          }
-      } else if constexpr (kAsync) {
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-          const bool in = pl.at(p, 0) < pl.m;
-          const uint32_t at = (uint32_t)(p * pl.width + pl.lane) * 16u;
-          float a[kPiece], b[kPiece];
-          unpack_piece(in ? slot_piece(slot_x + at) : make_uint4(0u, 0u, 0u, 0u), dt, a);
-          unpack_piece(in ? slot_piece(slot_x2 + at) : make_uint4(0u, 0u, 0u, 0u), dt, b);
-          gate_piece<P>(r, p, a, b, dt, top_lo, top_hi);
-        }
-      } else if constexpr (kVec) {
-        uint4 ra[P], rb[P];
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-          const size_t i = (size_t)pl.at(p, 0) * 2;
-          ra[p] = rb[p] = make_uint4(0u, 0u, 0u, 0u);
-          if (pl.at(p, 0) < pl.m) { ra[p] = *reinterpret_cast<const uint4*>(row_x(row) + i); rb[p] = *reinterpret_cast<const uint4*>(row_x2(row) + i); }
-        }
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-          float a[kPiece], b[kPiece];
-          unpack_piece(ra[p], dt, a);
-          unpack_piece(rb[p], dt, b);
-          gate_piece<P>(r, p, a, b, dt, top_lo, top_hi);
-        }
-      } else {
-        float a[P][kPiece], b[P][kPiece];
-        load_row<P, kVec>(pl, row_x(row), dt, a);
-        load_row<P, kVec>(pl, row_x2(row), dt, b);
-#pragma unroll
-        for (int p = 0; p < P; ++p) gate_piece<P>(r, p, a[p], b[p], dt, top_lo, top_hi);
       }
-      bits = row_max<kWarp>(magnitude_bits(top_lo, dt), sh, slot);
-      if constexpr (kIn == kInGated) {
-        if (row_max<kWarp>(magnitude_bits(top_hi, dt), sh, slot + 1) != bits) {       // the same for every thread of the row
-          top_lo = 0;
+      uint32_t largest = row_max<kWarp>(max(top >> 16, top & 0xFFFFu), sh, slot);
+      if constexpr (kGated) {
+        if (largest & 1u) {                         // the largest has two candidates (the same for every thread of the row)
+          top = 0;
 #pragma unroll
           for (int p = 0; p < P; ++p) {
             if ((r.marks >> (4 * p)) & 15u) settle(r, p, -1.0f, 0.0f);
 #pragma unroll
-            for (int k = 0; k < kPiece / 2; ++k) top_lo = max_sixteen(top_lo, r.h[p][k]);
+            for (int k = 0; k < kPiece / 2; ++k) top = __vmaxu2(top, r.h[p][k] & 0x7FFF7FFFu);
           }
           r.marks = 0;
-          bits = row_max<kWarp>(magnitude_bits(top_lo, dt), sh, slot + 2);
+          largest = 2u * row_max<kWarp>(max(top >> 16, top & 0xFFFFu), sh, slot + 1);
         }
+        largest >>= 1;
       }
+      bits = magnitude_bits<kType>(largest);
     }
     if (kAsync && row + stride < args.rows) ask(row + stride);        // (this row's pieces have been read: its largest magnitude is known)
     const RowScale s = row_scale(bits);
     int8_t* qr = args.q + (size_t)row * args.ldq;
     if (pl.lane == 0) args.scale[row] = s.scale;
-    if constexpr (kIn == kInWide) {
+    if constexpr (kType == STB_F32) {
       store_row_i8<P, kVec>(pl, qr, r.v, s);
     } else {
 #pragma unroll
       for (int p = 0; p < P; ++p) {
         if (pl.at(p, 0) >= pl.m) break;
         float v[kPiece];
-        auto unpack = [&]() {
+        unpack_piece<kType>(make_uint4(r.h[p][0], r.h[p][1], r.h[p][2], r.h[p][3]), v);
+        if (kGated && ((r.marks >> (4 * p)) & 15u)) {
+          // only a value that lies within a step of the 16-bit type of a border needs to be settled: 2^-10 (fp16) or 2^-7 of it, and 2^-24 (fp16) where that is less
+          constexpr float kStep = kType == STB_F16 ? 9.765625e-4f : 7.8125e-3f;
+          float near = 0.0f;
 #pragma unroll
-          for (int k = 0; k < kPiece / 2; ++k) unpack_two(r.h[p][k], dt, v[2 * k], v[2 * k + 1]);
-        };
-        unpack();
-        if constexpr (kIn == kInGated) {
-          // a step of the 16-bit type is at most 2^-10 (fp16) or 2^-7 of its value, and 2^-24 (fp16) where that is less
-          store_piece_i8<kVec>(pl, qr, p, v, s, dt == STB_F16 ? 9.765625e-4f : 7.8125e-3f, [&](float near) {
-            if (!((r.marks >> (4 * p)) & 15u) || near < 0.4998f - 6.0e-8f * s.inverse) return false;
+          for (int k = 0; k < kPiece; ++k) {
+            const float t = v[k] * s.inverse;
+            near = fmaxf(near, fmaf(fabsf(t), kStep, fabsf(t - rintf(t))));
+          }
+          if (near > 0.4998f - 6.0e-8f * s.inverse) {
             settle(r, p, s.inverse, s.largest);
-            unpack();
-            return true;
-          });
-        } else {
-          store_piece_i8<kVec>(pl, qr, p, v, s, 0.0f, [](float) { return false; });
+            unpack_piece<kType>(make_uint4(r.h[p][0], r.h[p][1], r.h[p][2], r.h[p][3]), v);
+          }
         }
+        store_piece_i8<kVec>(pl, qr, p, v, s);
       }
     }
   }
 }
 // A row that does not fit the registers of a CTA is read twice.
-template <bool kVec, bool kGated>
+template <int kType, bool kGated, bool kVec>
 __global__ void __launch_bounds__(kMaxRowThreads)
 quantize_i8_long_kernel(const QuantI8Args args) {
   __shared__ float sh[1][32];
   const void *x = args.x, *x2 = args.x2;
   begin_after(x, x2);
-  const int dt = args.dt, bytes = dtype_bytes(dt), row = (int)blockIdx.x, span = kMaxRowThreads * kPiece;
-  const char *xr = static_cast<const char*>(x) + (size_t)row * args.ldx * (size_t)bytes, *xr2 = static_cast<const char*>(x2) + (size_t)row * args.ldx2 * (size_t)bytes;
+  constexpr int kBytes = kType == STB_F32 ? 4 : 2, kSpan = kMaxRowThreads * kPiece;
+  const int row = (int)blockIdx.x;
+  const char *xr = static_cast<const char*>(x) + (size_t)row * args.ldx * kBytes, *xr2 = static_cast<const char*>(x2) + (size_t)row * args.ldx2 * kBytes;
   RowPlace<kVec> pl{(int)threadIdx.x, kMaxRowThreads, args.m};
   float v[1][kPiece];
   auto read = [&](int base) {
     pl.m = args.m - base;
-    load_row<1, kVec>(pl, xr + (size_t)base * bytes, dt, v);
-    if (kGated) {
-      float b[1][kPiece];
-      load_row<1, kVec>(pl, xr2 + (size_t)base * bytes, dt, b);
+    values_of<kType>(load_piece<kType, kVec>(pl, xr + (size_t)base * kBytes, 0), v[0]);
+    if constexpr (kGated) {
+      float b[kPiece];
+      values_of<kType>(load_piece<kType, kVec>(pl, xr2 + (size_t)base * kBytes, 0), b);
 #pragma unroll
       for (int k = 0; k < kPiece; k += 2) {
         uint32_t lo, hi;
-        gated_two(v[0][k], v[0][k + 1], b[0][k], b[0][k + 1], dt, lo, hi);
-        if (lo != hi || fminf(v[0][k], v[0][k + 1]) < -80.0f) lo = gated_exact(v[0][k], v[0][k + 1], b[0][k], b[0][k + 1], dt);
-        unpack_two(lo, dt, v[0][k], v[0][k + 1]);
+        gated_two<kType>(v[0][k], v[0][k + 1], b[k], b[k + 1], lo, hi);
+        if (lo != hi || fminf(v[0][k], v[0][k + 1]) < -80.0f) lo = gated_exact<kType>(v[0][k], v[0][k + 1], b[k], b[k + 1]);
+        unpack_two<kType>(lo, v[0][k], v[0][k + 1]);
       }
     }
   };
   uint32_t bits = 0;
-  for (int base = 0; base < args.m; base += span) { read(base); bits = max(bits, max_bits<1>(v)); if (args.m - base <= span) break; }
+  for (int base = 0;; base += kSpan) { read(base); bits = max(bits, max_bits<1>(v)); if (args.m - base <= kSpan) break; }
   const RowScale s = row_scale(row_max<false>(bits, sh, 0));
   if (threadIdx.x == 0) args.scale[row] = s.scale;
-  for (int base = 0; base < args.m; base += span) {
+  for (int base = 0;; base += kSpan) {
     read(base);
     store_row_i8<1, kVec>(pl, args.q + (size_t)row * args.ldq + base, v, s);
-    if (args.m - base <= span) break;
+    if (args.m - base <= kSpan) break;
   }
 }
 
@@ -573,25 +590,13 @@ __device__ __forceinline__ void norm_row(const RowPlace<kVec>& pl, float (&v)[P]
 #pragma unroll
     for (int k = 0; k < kPiece; ++k) v[p][k] *= inv;
 }
-// v = f(v, the row at w), piece by piece
+// v = f(v, the row at w)
 template <int P, bool kVec, class F>
 __device__ __forceinline__ void with_row(const RowPlace<kVec>& pl, float (&v)[P][kPiece], const void* w, int dt, F f) {
-  auto piece = [&](int p, int type) {
-    RowPlace<kVec> one = pl;
-    float u[1][kPiece];
-    if (kVec) one.lane += p * pl.width;
-    else one.lane += p * kPiece * pl.width;
-    load_row<1, kVec>(one, w, type, u);
+  for_row<P, kVec>(pl, w, dt, [&](int p, const float (&u)[kPiece]) {
 #pragma unroll
-    for (int k = 0; k < kPiece; ++k) v[p][k] = f(v[p][k], u[0][k]);
-  };
-  if (dt == STB_F32) {
-#pragma unroll
-    for (int p = 0; p < P; ++p) piece(p, STB_F32);
-  } else {
-#pragma unroll
-    for (int p = 0; p < P; ++p) piece(p, dt);
-  }
+    for (int k = 0; k < kPiece; ++k) v[p][k] = f(v[p][k], u[k]);
+  });
 }
 template <int P, bool kVec, bool kWarp, bool kAsync>
 __global__ void __launch_bounds__(kWarp ? 256 : (kAsync ? 512 : kMaxRowThreads), kWarp || (kAsync && P <= 4) ? 2 : 1)
@@ -617,7 +622,10 @@ block_norm_kernel(const __grid_constant__ stb_norm a) {
     float v[P][kPiece], r[kEarly ? P : 1][kPiece];
     if constexpr (kAsync) {
       copy_async_done();
-      take_row<P>(pl, a.xdt, slot_x, v);
+      for_slots<P>(pl, a.xdt, slot_x, [&](int p, const float (&u)[kPiece]) {
+#pragma unroll
+        for (int k = 0; k < kPiece; ++k) v[p][k] = u[k];
+      });
     } else {
       load_row<P, kVec>(pl, row_of(x, row, a.ldx, a.xdt), a.xdt, v);
       if constexpr (kEarly) {
@@ -643,12 +651,10 @@ block_norm_kernel(const __grid_constant__ stb_norm a) {
 #pragma unroll
         for (int k = 0; k < kPiece; ++k) v[p][k] = fmaf(a.alpha, v[p][k], r[p][k]);
     } else if constexpr (kAsync) {
+      for_slots<P>(pl, a.rdt, slot_r, [&](int p, const float (&u)[kPiece]) {
 #pragma unroll
-      for (int p = 0; p < P; ++p) {
-        take_piece(pl, p, a.rdt, slot_r, r[0]);
-#pragma unroll
-        for (int k = 0; k < kPiece; ++k) v[p][k] = fmaf(a.alpha, v[p][k], r[0][k]);
-      }
+        for (int k = 0; k < kPiece; ++k) v[p][k] = fmaf(a.alpha, v[p][k], u[k]);
+      });
     } else {
       with_row<P, kVec>(pl, v, row_of(resid, row, a.ldr, a.rdt), a.rdt, [&](float u, float f) { return fmaf(a.alpha, u, f); });
     }
@@ -674,11 +680,12 @@ block_norm_kernel(const __grid_constant__ stb_norm a) {
 // ---- launches -----------------------------------------------------------------------------------------------------------------------
 // How rows of m values are dealt out.
 //   warp:    rows of up to 256 values, or of up to 1024 where there are more than SMs; 1 or 4 pieces per lane
-//   async:   more than 296 rows that can be read in 16-byte pieces: 4 pieces per thread (8 beyond 16384 values), as many CTAs as stay on the GPU
+//   async:   more than 296 rows that can be read in 16-byte pieces: 4 or 8 pieces per thread, whichever fills an SM better (resident4, resident8: the
+//            threads that its registers take), as many CTAs as stay on the GPU
 //   else:    one CTA per row, with one piece per thread as long as 1024 threads reach, for the shortest way through a row
 enum RowForm { kRowWarp, kRowAsync, kRowDirect, kRowLong };
 struct RowShape { RowForm form; int pieces, threads, grid; uint32_t smem; };
-static RowShape row_shape(int m, int rows, bool vec, uint32_t slot_bytes_per_piece, uint32_t static_smem) {
+static RowShape row_shape(int m, int rows, bool vec, uint32_t slot_bytes_per_piece, uint32_t static_smem, int resident4, int resident8) {
   RowShape s = {};
   const int pieces = (m + kPiece - 1) / kPiece;
   if (m > kMaxRow) { s.form = kRowLong; s.pieces = 1; s.threads = kMaxRowThreads; s.grid = rows; return s; }
@@ -691,15 +698,20 @@ static RowShape row_shape(int m, int rows, bool vec, uint32_t slot_bytes_per_pie
     return s;
   }
   if (vec && rows > 296) {
-    s.form = kRowAsync;
-    s.pieces = pieces <= 4 * 512 ? 4 : 8;
-    s.threads = ((pieces + s.pieces - 1) / s.pieces + 31) / 32 * 32;
+    const int threads4 = ((pieces + 3) / 4 + 31) / 32 * 32, threads8 = ((pieces + 7) / 8 + 31) / 32 * 32;
+    const bool four = threads4 <= 512 && resident4 / threads4 * threads4 >= resident8 / threads8 * threads8;      // threads that an SM holds
+    s.pieces = four ? 4 : 8;
+    s.threads = four ? threads4 : threads8;
     s.smem = (uint32_t)(s.pieces * s.threads) * slot_bytes_per_piece;
-    int resident = 1024 / s.threads, by_smem = (int)(228u * 1024u / (s.smem + 1024u + static_smem));
-    if (resident > by_smem) resident = by_smem;
-    if (resident < 1) resident = 1;
-    s.grid = rows < 148 * resident ? rows : 148 * resident;
-    return s;
+    if (s.smem <= (uint32_t)kMaxRowSmem) {          // (not two inputs of fp32 beyond 28672 values)
+      int resident = (four ? resident4 : resident8) / s.threads, by_smem = (int)(228u * 1024u / (s.smem + 1024u + static_smem));
+      if (resident > by_smem) resident = by_smem;
+      if (resident < 1) resident = 1;
+      s.form = kRowAsync;
+      s.grid = rows < 148 * resident ? rows : 148 * resident;
+      return s;
+    }
+    s.smem = 0;
   }
   s.form = kRowDirect;
   s.pieces = pieces <= kMaxRowThreads ? 1 : (pieces <= 2 * kMaxRowThreads ? 2 : 4);
@@ -712,37 +724,37 @@ static bool rows_aligned(const void* p, size_t ld, int bytes, size_t to) { retur
 static bool element_aligned(const void* p, int dt) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(dtype_bytes(dt) - 1)) == 0; }
 static bool known_dtype(int dt) { return dt == STB_F16 || dt == STB_BF16 || dt == STB_F32; }
 
-// A kernel with more than 48 KB of shared memory has to be allowed it, on every device.
-template <typename K, typename A>
-static cudaError_t launch_rows(K kernel, const RowShape& s, cudaStream_t st, const A& args) {
-  if (s.smem > 48 * 1024) {
+// A kernel with more than 48 KB of shared memory (what it declares included) has to be allowed it, on every device.
+template <auto kKernel, typename A>
+static cudaError_t launch_rows(const RowShape& s, cudaStream_t st, const A& args) {
+  if (s.smem > 46 * 1024) {
     static bool done[64] = {};
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= 64 || !done[dev]) {
-      e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 228 * 1024 - 4096);
+      e = cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxRowSmem);
       if (e != cudaSuccess) return e;
       if (dev >= 0 && dev < 64) done[dev] = true;
     }
   }
-  return launch_after(kernel, dim3((unsigned)s.grid), dim3((unsigned)s.threads), s.smem, st, args);
+  return launch_after(kKernel, dim3((unsigned)s.grid), dim3((unsigned)s.threads), s.smem, st, args);
 }
 
-template <int kIn>
+template <int kType, bool kGated>
 static cudaError_t launch_quantize(const QuantI8Args& a, const RowShape& s, bool vec, cudaStream_t st) {
   switch (s.form) {
     case kRowLong:
-      return vec ? launch_rows(quantize_i8_long_kernel<true, kIn == kInGated>, s, st, a) : launch_rows(quantize_i8_long_kernel<false, kIn == kInGated>, s, st, a);
+      return vec ? launch_rows<quantize_i8_long_kernel<kType, kGated, true>>(s, st, a) : launch_rows<quantize_i8_long_kernel<kType, kGated, false>>(s, st, a);
     case kRowWarp:
-      if (s.pieces == 1) return vec ? launch_rows(quantize_i8_kernel<1, kIn, true, true, false>, s, st, a) : launch_rows(quantize_i8_kernel<1, kIn, false, true, false>, s, st, a);
-      return vec ? launch_rows(quantize_i8_kernel<4, kIn, true, true, false>, s, st, a) : launch_rows(quantize_i8_kernel<4, kIn, false, true, false>, s, st, a);
+      if (s.pieces == 1) return vec ? launch_rows<quantize_i8_kernel<1, kType, kGated, true, true, false>>(s, st, a) : launch_rows<quantize_i8_kernel<1, kType, kGated, false, true, false>>(s, st, a);
+      return vec ? launch_rows<quantize_i8_kernel<4, kType, kGated, true, true, false>>(s, st, a) : launch_rows<quantize_i8_kernel<4, kType, kGated, false, true, false>>(s, st, a);
     case kRowAsync:
-      return s.pieces == 4 ? launch_rows(quantize_i8_kernel<4, kIn, true, false, true>, s, st, a) : launch_rows(quantize_i8_kernel<8, kIn, true, false, true>, s, st, a);
+      return s.pieces == 4 ? launch_rows<quantize_i8_kernel<4, kType, kGated, true, false, true>>(s, st, a) : launch_rows<quantize_i8_kernel<8, kType, kGated, true, false, true>>(s, st, a);
     default:
-      if (s.pieces == 1) return vec ? launch_rows(quantize_i8_kernel<1, kIn, true, false, false>, s, st, a) : launch_rows(quantize_i8_kernel<1, kIn, false, false, false>, s, st, a);
-      if (s.pieces == 2) return vec ? launch_rows(quantize_i8_kernel<2, kIn, true, false, false>, s, st, a) : launch_rows(quantize_i8_kernel<2, kIn, false, false, false>, s, st, a);
-      return vec ? launch_rows(quantize_i8_kernel<4, kIn, true, false, false>, s, st, a) : launch_rows(quantize_i8_kernel<4, kIn, false, false, false>, s, st, a);
+      if (s.pieces == 1) return vec ? launch_rows<quantize_i8_kernel<1, kType, kGated, true, false, false>>(s, st, a) : launch_rows<quantize_i8_kernel<1, kType, kGated, false, false, false>>(s, st, a);
+      if (s.pieces == 2) return vec ? launch_rows<quantize_i8_kernel<2, kType, kGated, true, false, false>>(s, st, a) : launch_rows<quantize_i8_kernel<2, kType, kGated, false, false, false>>(s, st, a);
+      return vec ? launch_rows<quantize_i8_kernel<4, kType, kGated, true, false, false>>(s, st, a) : launch_rows<quantize_i8_kernel<4, kType, kGated, false, false, false>>(s, st, a);
   }
 }
 
@@ -757,13 +769,17 @@ extern "C" int stb_quantize_i8(const void* x, size_t ldx, const void* x2, size_t
   if (!stb::element_aligned(x, xdt) || !stb::element_aligned(x2, xdt) || !stb::element_aligned(scale, STB_F32)) return STB_ERR_ARG;
   const int bytes = stb::dtype_bytes(xdt);
   const bool vec = m % stb::kPiece == 0 && stb::rows_aligned(x, ldx, bytes, 16) && stb::rows_aligned(x2, ldx2, bytes, 16) && stb::rows_aligned(q, ldq, 1, 8);
-  const stb::QuantI8Args a = {x, x2, xdt, rows, m, ldx, ldx2, ldq, q, scale};
-  const stb::RowShape s = stb::row_shape(m, rows, vec, xdt == STB_F32 || x2 ? 32u : 16u, 6u * 128u);
+  const stb::QuantI8Args a = {x, x2, rows, m, ldx, ldx2, ldq, q, scale};
+  const stb::RowShape s = stb::row_shape(m, rows, vec, xdt == STB_F32 || x2 ? 32u : 16u, 4u * 128u, 1024, xdt == STB_F32 ? 512 : 1024);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = x2 ? stb::launch_quantize<stb::kInGated>(a, s, vec, st)
-                           : (xdt == STB_F32 ? stb::launch_quantize<stb::kInWide>(a, s, vec, st) : stb::launch_quantize<stb::kInSixteen>(a, s, vec, st));
+  const bool half = xdt == STB_F16;
+  const cudaError_t e = x2 ? (half ? stb::launch_quantize<STB_F16, true>(a, s, vec, st) : stb::launch_quantize<STB_BF16, true>(a, s, vec, st))
+                           : (xdt == STB_F32 ? stb::launch_quantize<STB_F32, false>(a, s, vec, st)
+                                             : (half ? stb::launch_quantize<STB_F16, false>(a, s, vec, st) : stb::launch_quantize<STB_BF16, false>(a, s, vec, st)));
   return e == cudaSuccess ? STB_OK : STB_ERR_CUDA;
 }
+
+static int status(cudaError_t e) { return e == cudaSuccess ? STB_OK : STB_ERR_CUDA; }
 
 extern "C" int stb_block_norm(const stb_norm* args, void* stream) {
   if (!args) return STB_ERR_ARG;
@@ -791,18 +807,17 @@ extern "C" int stb_block_norm(const stb_norm* args, void* stream) {
                    stb::rows_aligned(a.post_weight, 0, wb, 16) && stb::rows_aligned(a.post_bias, 0, wb, 16) && stb::rows_aligned(a.weight, 0, wb, 16) &&
                    stb::rows_aligned(a.bias, 0, wb, 16);
   const uint32_t slot = (a.xdt == STB_F32 ? 32u : 16u) + (!a.resid ? 0u : (a.rdt == STB_F32 ? 32u : 16u));
-  const stb::RowShape s = stb::row_shape(a.h, a.tokens, vec, slot, 10u * 128u);
+  const stb::RowShape s = stb::row_shape(a.h, a.tokens, vec, slot, 10u * 128u, 1024, 512);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  auto go = [&](auto kernel) { return stb::launch_rows(kernel, s, st, a) == cudaSuccess ? STB_OK : STB_ERR_CUDA; };
   switch (s.form) {
     case stb::kRowWarp:
-      if (s.pieces == 1) return vec ? go(stb::block_norm_kernel<1, true, true, false>) : go(stb::block_norm_kernel<1, false, true, false>);
-      return vec ? go(stb::block_norm_kernel<4, true, true, false>) : go(stb::block_norm_kernel<4, false, true, false>);
+      if (s.pieces == 1) return vec ? status(stb::launch_rows<stb::block_norm_kernel<1, true, true, false>>(s, st, a)) : status(stb::launch_rows<stb::block_norm_kernel<1, false, true, false>>(s, st, a));
+      return vec ? status(stb::launch_rows<stb::block_norm_kernel<4, true, true, false>>(s, st, a)) : status(stb::launch_rows<stb::block_norm_kernel<4, false, true, false>>(s, st, a));
     case stb::kRowAsync:
-      return s.pieces == 4 ? go(stb::block_norm_kernel<4, true, false, true>) : go(stb::block_norm_kernel<8, true, false, true>);
+      return s.pieces == 4 ? status(stb::launch_rows<stb::block_norm_kernel<4, true, false, true>>(s, st, a)) : status(stb::launch_rows<stb::block_norm_kernel<8, true, false, true>>(s, st, a));
     default:
-      if (s.pieces == 1) return vec ? go(stb::block_norm_kernel<1, true, false, false>) : go(stb::block_norm_kernel<1, false, false, false>);
-      if (s.pieces == 2) return vec ? go(stb::block_norm_kernel<2, true, false, false>) : go(stb::block_norm_kernel<2, false, false, false>);
-      return vec ? go(stb::block_norm_kernel<4, true, false, false>) : go(stb::block_norm_kernel<4, false, false, false>);
+      if (s.pieces == 1) return vec ? status(stb::launch_rows<stb::block_norm_kernel<1, true, false, false>>(s, st, a)) : status(stb::launch_rows<stb::block_norm_kernel<1, false, false, false>>(s, st, a));
+      if (s.pieces == 2) return vec ? status(stb::launch_rows<stb::block_norm_kernel<2, true, false, false>>(s, st, a)) : status(stb::launch_rows<stb::block_norm_kernel<2, false, false, false>>(s, st, a));
+      return vec ? status(stb::launch_rows<stb::block_norm_kernel<4, true, false, false>>(s, st, a)) : status(stb::launch_rows<stb::block_norm_kernel<4, false, false, false>>(s, st, a));
   }
 }

@@ -61,9 +61,9 @@ def _same(a, b):
 
 
 def _check_rows(q, scale, v):
-    want_q, want_s = _rows64(v)
-    assert torch.equal(q.cpu().double(), want_q)
-    assert _same(scale.cpu(), want_s.float())
+    want_q, want_s = _rows64(v.cuda())
+    assert torch.equal(q.double(), want_q)
+    assert _same(scale.cpu(), want_s.float().cpu())
 
 
 # ---- without a GPU: what is refused ---------------------------------------------------------------------------------------------------
@@ -145,6 +145,23 @@ def test_gated_rows_in_8_bits(stb, m, dt):
         b[0] = 0
         for q, s in (stb.quantize_i8(a.cuda(), b.cuda()), stb.quantize_i8(_place(a, 8, 8), _place(b, 5, 3))):
             _check_rows(q, s, _gated64(a, b))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m", (264, 1032, 2816, 4096, 5120, 6008, 8192, 11008, 12000, 12288, 13824, 16384, 16392, 20480, 24568, 28672, 32768))
+def test_many_rows(stb, m):
+    """More rows than stay on the GPU at once, of every width class: each CTA or warp takes several."""
+    for k, dt in enumerate(("f16", "bf16", "f32")):
+        rows = 310 + 700 * ((m + k) % 3 == 0)
+        x = _values(rows, m, m + k, dt)
+        x[7] = 0
+        x[rows - 1, m - 1] = 300.0
+        _check_rows(*stb.quantize_i8(x.cuda()), x)
+        if dt != "f32":
+            b = _values(rows, m, m + k + 9, dt)
+            _check_rows(*stb.quantize_i8(x.cuda(), b.cuda()), _gated64(x.cuda(), b.cuda()).cpu())
+    for k, kw in enumerate((dict(x="f16", r="f16", w="f16", y="bf16"), dict(x="f32", r="f32", w="f32", y="i8", kind="layer", bias=True), dict(x="bf16", r=None, post=True, w="f32", y="f32", gate=2))):
+        _check_norm(stb, 310 + 200 * k, m, m + k, **kw)
 
 
 @pytest.mark.gpu
