@@ -330,6 +330,12 @@ __device__ __forceinline__ void store_row_i8(const RowPlace<kVec>& pl, int8_t* r
 // fp32 rounding half a one each; a >= -80, where nothing leaves fp32's range): both ends of a band somewhat wider are rounded, and nearly always give the same 16-bit value.  Where they
 // do not, that of the smaller magnitude is kept, the other is the next one up, and the pair is marked: it is evaluated in float64 only where the
 // choice would show, in the row's largest magnitude or in the value's 8 bits.
+// the larger of each half
+__device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
 template <int kType>
 __device__ __noinline__ uint32_t gated_exact(float a0, float a1, float b0, float b1) {
   const double d0 = (double)a0, d1 = (double)a1;
@@ -387,24 +393,35 @@ __device__ __noinline__ uint4 settle_piece(uint4 h, uint32_t marks, const void* 
   }
   return h;
 }
+template <int kType>
+__device__ __noinline__ uint4 gated_exact_piece(uint4 ra, uint4 rb) {
+  float a[kPiece], b[kPiece];
+  unpack_piece<kType>(ra, a);
+  unpack_piece<kType>(rb, b);
+  return make_uint4(gated_exact<kType>(a[0], a[1], b[0], b[1]), gated_exact<kType>(a[2], a[3], b[2], b[3]), gated_exact<kType>(a[4], a[5], b[4], b[5]), gated_exact<kType>(a[6], a[7], b[6], b[7]));
+}
 // The gated values of a piece.  top: per half the largest of 2 magnitude + (whether there are two candidates), of the larger candidates.
 template <int P, int kType>
 __device__ __forceinline__ void gate_piece(QuantRow<P, kType>& r, int p, const uint4& ra, const uint4& rb, uint32_t& top) {
   float a[kPiece], b[kPiece];
   unpack_piece<kType>(ra, a);
   unpack_piece<kType>(rb, b);
+  uint32_t lo[kPiece / 2], hi[kPiece / 2];
   float least = a[0];
 #pragma unroll
   for (int k = 1; k < kPiece; ++k) least = fminf(least, a[k]);
 #pragma unroll
+  for (int k = 0; k < kPiece / 2; ++k) gated_two<kType>(a[2 * k], a[2 * k + 1], b[2 * k], b[2 * k + 1], lo[k], hi[k]);
+  if (least < -80.0f) {
+    const uint4 e = gated_exact_piece<kType>(ra, rb);
+    lo[0] = hi[0] = e.x; lo[1] = hi[1] = e.y; lo[2] = hi[2] = e.z; lo[3] = hi[3] = e.w;
+  }
+#pragma unroll
   for (int k = 0; k < kPiece / 2; ++k) {
-    uint32_t lo, hi;
-    gated_two<kType>(a[2 * k], a[2 * k + 1], b[2 * k], b[2 * k + 1], lo, hi);
-    if (least < -80.0f) lo = hi = gated_exact<kType>(a[2 * k], a[2 * k + 1], b[2 * k], b[2 * k + 1]);
-    r.h[p][k] = lo;
-    const bool two = ((lo ^ hi) & 0x7FFF7FFFu) != 0u;      // (a zero's sign says nothing)
+    const bool two = ((lo[k] ^ hi[k]) & 0x7FFF7FFFu) != 0u;      // (a zero's sign says nothing)
+    r.h[p][k] = lo[k];
     if (two) r.marks |= 1u << (4 * p + k);
-    top = __vmaxu2(top, ((hi << 1) & 0xFFFEFFFEu) | (two ? 0x00010001u : 0u));
+    top = max_halves(top, ((hi[k] << 1) & 0xFFFEFFFEu) | (two ? 0x00010001u : 0u));
   }
 }
 // fp32 bits of a 16-bit magnitude
@@ -416,7 +433,7 @@ __device__ __forceinline__ uint32_t magnitude_bits(uint32_t m) {
 }
 // kWarp: a row belongs to a warp, else to the CTA, which takes every gridDim-th one.  kAsync: the pieces of the next row are on their way.
 template <int P, int kType, bool kGated, bool kVec, bool kWarp, bool kAsync>
-__global__ void __launch_bounds__(kWarp ? 256 : (kAsync ? 512 : kMaxRowThreads), kWarp || (kAsync && (P <= 4 || kType != STB_F32)) ? 2 : 1)
+__global__ void __launch_bounds__(kWarp ? 256 : (kAsync && !kGated ? 512 : kMaxRowThreads), kWarp || (kAsync && !kGated && (P <= 4 || kType != STB_F32)) ? 2 : 1)
 quantize_i8_kernel(const QuantI8Args args) {
   extern __shared__ __align__(16) uint8_t slots[];
   __shared__ float sh[4][32];                       // the parts of a row's two reductions, and of the next one's
@@ -474,7 +491,7 @@ quantize_i8_kernel(const QuantI8Args args) {
         } else {
           r.h[p][0] = raw[p].w[0].x; r.h[p][1] = raw[p].w[0].y; r.h[p][2] = raw[p].w[0].z; r.h[p][3] = raw[p].w[0].w;
 #pragma unroll
-          for (int k = 0; k < kPiece / 2; ++k) top = __vmaxu2(top, r.h[p][k] & 0x7FFF7FFFu);
+          for (int k = 0; k < kPiece / 2; ++k) top = max_halves(top, r.h[p][k] & 0x7FFF7FFFu);
         }
       }
       uint32_t largest = row_max<kWarp>(max(top >> 16, top & 0xFFFFu), sh, slot);
@@ -485,7 +502,7 @@ quantize_i8_kernel(const QuantI8Args args) {
           for (int p = 0; p < P; ++p) {
             if ((r.marks >> (4 * p)) & 15u) settle(r, p, -1.0f, 0.0f);
 #pragma unroll
-            for (int k = 0; k < kPiece / 2; ++k) top = __vmaxu2(top, r.h[p][k] & 0x7FFF7FFFu);
+            for (int k = 0; k < kPiece / 2; ++k) top = max_halves(top, r.h[p][k] & 0x7FFF7FFFu);
           }
           r.marks = 0;
           largest = 2u * row_max<kWarp>(max(top >> 16, top & 0xFFFFu), sh, slot + 1);
@@ -685,7 +702,7 @@ block_norm_kernel(const __grid_constant__ stb_norm a) {
 //   else:    one CTA per row, with one piece per thread as long as 1024 threads reach, for the shortest way through a row
 enum RowForm { kRowWarp, kRowAsync, kRowDirect, kRowLong };
 struct RowShape { RowForm form; int pieces, threads, grid; uint32_t smem; };
-static RowShape row_shape(int m, int rows, bool vec, uint32_t slot_bytes_per_piece, uint32_t static_smem, int resident4, int resident8) {
+static RowShape row_shape(int m, int rows, bool vec, uint32_t slot_bytes_per_piece, uint32_t static_smem, int resident4, int resident8, int most4 = 512) {
   RowShape s = {};
   const int pieces = (m + kPiece - 1) / kPiece;
   if (m > kMaxRow) { s.form = kRowLong; s.pieces = 1; s.threads = kMaxRowThreads; s.grid = rows; return s; }
@@ -699,7 +716,7 @@ static RowShape row_shape(int m, int rows, bool vec, uint32_t slot_bytes_per_pie
   }
   if (vec && rows > 296) {
     const int threads4 = ((pieces + 3) / 4 + 31) / 32 * 32, threads8 = ((pieces + 7) / 8 + 31) / 32 * 32;
-    const bool four = threads4 <= 512 && resident4 / threads4 * threads4 >= resident8 / threads8 * threads8;      // threads that an SM holds
+    const bool four = threads4 <= most4 && resident4 / threads4 * threads4 >= resident8 / threads8 * threads8;      // threads that an SM holds
     s.pieces = four ? 4 : 8;
     s.threads = four ? threads4 : threads8;
     s.smem = (uint32_t)(s.pieces * s.threads) * slot_bytes_per_piece;
@@ -750,7 +767,10 @@ static cudaError_t launch_quantize(const QuantI8Args& a, const RowShape& s, bool
       if (s.pieces == 1) return vec ? launch_rows<quantize_i8_kernel<1, kType, kGated, true, true, false>>(s, st, a) : launch_rows<quantize_i8_kernel<1, kType, kGated, false, true, false>>(s, st, a);
       return vec ? launch_rows<quantize_i8_kernel<4, kType, kGated, true, true, false>>(s, st, a) : launch_rows<quantize_i8_kernel<4, kType, kGated, false, true, false>>(s, st, a);
     case kRowAsync:
-      return s.pieces == 4 ? launch_rows<quantize_i8_kernel<4, kType, kGated, true, false, true>>(s, st, a) : launch_rows<quantize_i8_kernel<8, kType, kGated, true, false, true>>(s, st, a);
+      if constexpr (!kGated) {
+        if (s.pieces == 8) return launch_rows<quantize_i8_kernel<8, kType, kGated, true, false, true>>(s, st, a);
+      }
+      return launch_rows<quantize_i8_kernel<4, kType, kGated, true, false, true>>(s, st, a);
     default:
       if (s.pieces == 1) return vec ? launch_rows<quantize_i8_kernel<1, kType, kGated, true, false, false>>(s, st, a) : launch_rows<quantize_i8_kernel<1, kType, kGated, false, false, false>>(s, st, a);
       if (s.pieces == 2) return vec ? launch_rows<quantize_i8_kernel<2, kType, kGated, true, false, false>>(s, st, a) : launch_rows<quantize_i8_kernel<2, kType, kGated, false, false, false>>(s, st, a);
@@ -770,7 +790,7 @@ extern "C" int stb_quantize_i8(const void* x, size_t ldx, const void* x2, size_t
   const int bytes = stb::dtype_bytes(xdt);
   const bool vec = m % stb::kPiece == 0 && stb::rows_aligned(x, ldx, bytes, 16) && stb::rows_aligned(x2, ldx2, bytes, 16) && stb::rows_aligned(q, ldq, 1, 8);
   const stb::QuantI8Args a = {x, x2, rows, m, ldx, ldx2, ldq, q, scale};
-  const stb::RowShape s = stb::row_shape(m, rows, vec, xdt == STB_F32 || x2 ? 32u : 16u, 4u * 128u, 1024, xdt == STB_F32 ? 512 : 1024);
+  const stb::RowShape s = stb::row_shape(m, rows, vec, xdt == STB_F32 || x2 ? 32u : 16u, 4u * 128u, 1024, x2 ? 0 : (xdt == STB_F32 ? 512 : 1024), x2 ? 1024 : 512);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool half = xdt == STB_F16;
   const cudaError_t e = x2 ? (half ? stb::launch_quantize<STB_F16, true>(a, s, vec, st) : stb::launch_quantize<STB_BF16, true>(a, s, vec, st))
