@@ -27,6 +27,18 @@ constexpr float kSmallestMax = 3.0092655e-36f;      // 2^-118: below it 127 / ma
 
 __host__ __device__ inline int dtype_bytes(int dt) { return dt == STB_F32 ? 4 : 2; }
 
+// ---- two fp32 operations in one instruction ------------------------------------------------------------------------------------------
+__device__ __forceinline__ void mul_two(float& d0, float& d1, float a0, float a1, float b0, float b1) {
+  asm("{\n\t.reg .b64 a, b;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 a, a, b;\n\tmov.b64 {%0, %1}, a;\n\t}" : "=f"(d0), "=f"(d1) : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
+}
+__device__ __forceinline__ void add_two(float& d0, float& d1, float a0, float a1, float b0, float b1) {
+  asm("{\n\t.reg .b64 a, b;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 a, a, b;\n\tmov.b64 {%0, %1}, a;\n\t}" : "=f"(d0), "=f"(d1) : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
+}
+__device__ __forceinline__ void fma_two(float& d0, float& d1, float a0, float a1, float b0, float b1, float c0, float c1) {
+  asm("{\n\t.reg .b64 a, b, c;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\tfma.rn.f32x2 a, a, b, c;\n\tmov.b64 {%0, %1}, a;\n\t}"
+      : "=f"(d0), "=f"(d1) : "f"(a0), "f"(a1), "f"(b0), "f"(b1), "f"(c0), "f"(c1));
+}
+
 // ---- a thread's values of a row ------------------------------------------------------------------------------------------------------
 // Piece p of thread `lane` of `width` is the eight values at 8 (p width + lane) where rows can be read in 16-byte pieces (their length a multiple
 // of 8), else every value is width behind the one before it, so that a warp's loads stay together.
@@ -298,10 +310,14 @@ __device__ __forceinline__ void store_piece_i8(const RowPlace<kVec>& pl, int8_t*
   uint32_t q[kPiece];
   float off = 0.0f;                                 // the farthest from a whole number: 0.5 is a border
 #pragma unroll
-  for (int k = 0; k < kPiece; ++k) {
-    const float u = fmaf(v[k], s.inverse, kRoundBias);
-    off = fmaxf(off, fabsf(fmaf(v[k], s.inverse, -(u - kRoundBias))));
-    q[k] = __float_as_uint(u);
+  for (int k = 0; k < kPiece; k += 2) {
+    float u0, u1, r0, r1, d0, d1;
+    fma_two(u0, u1, v[k], v[k + 1], s.inverse, s.inverse, kRoundBias, kRoundBias);
+    add_two(r0, r1, u0, u1, -kRoundBias, -kRoundBias);
+    fma_two(d0, d1, v[k], v[k + 1], -s.inverse, -s.inverse, r0, r1);
+    off = fmaxf(off, fmaxf(fabsf(d0), fabsf(d1)));
+    q[k] = __float_as_uint(u0);
+    q[k + 1] = __float_as_uint(u1);
   }
   uint2 two = make_uint2(__byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410),
                          __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410));
@@ -342,18 +358,22 @@ __device__ __noinline__ uint32_t gated_exact(float a0, float a1, float b0, float
   return pack_two<kType>((float)(d0 / (1.0 + exp(-d0)) * (double)b0), (float)(d1 / (1.0 + exp(-d1)) * (double)b1));
 }
 constexpr float kUlp = 1.1920929e-7f;               // 2^-23
-__device__ __forceinline__ float gated_one(float a, float b) {
-  float e, r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(a * -1.4426950408889634f));
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
-  return a * r * b;
-}
 template <int kType>
 __device__ __forceinline__ void gated_two(float a0, float a1, float b0, float b1, uint32_t& lo, uint32_t& hi) {
-  const float h0 = gated_one(a0, b0), h1 = gated_one(a1, b1);
-  const float band0 = fmaf(fminf(a0, 0.0f), -kUlp, 6.0f * kUlp), band1 = fmaf(fminf(a1, 0.0f), -kUlp, 6.0f * kUlp);
-  lo = pack_two<kType>(fmaf(-h0, band0, h0), fmaf(-h1, band1, h1));
-  hi = pack_two<kType>(fmaf(h0, band0, h0), fmaf(h1, band1, h1));
+  float t0, t1, h0, h1, band0, band1, l0, l1, m0, m1;
+  mul_two(t0, t1, a0, a1, -1.4426950408889634f, -1.4426950408889634f);
+  asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(t0));
+  asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(t1));
+  add_two(t0, t1, t0, t1, 1.0f, 1.0f);
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(t0));
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(t1));
+  mul_two(h0, h1, a0, a1, t0, t1);
+  mul_two(h0, h1, h0, h1, b0, b1);
+  fma_two(band0, band1, fminf(a0, 0.0f), fminf(a1, 0.0f), -kUlp, -kUlp, 6.0f * kUlp, 6.0f * kUlp);
+  fma_two(m0, m1, h0, h1, band0, band1, h0, h1);
+  fma_two(l0, l1, h0, h1, -band0, -band1, h0, h1);
+  lo = pack_two<kType>(l0, l1);
+  hi = pack_two<kType>(m0, m1);
 }
 
 // ---- stb_quantize_i8 ----------------------------------------------------------------------------------------------------------------
@@ -596,23 +616,23 @@ __device__ __forceinline__ void norm_row(const RowPlace<kVec>& pl, float (&v)[P]
 #pragma unroll
       for (int k = 0; k < kPiece; ++k) v[p][k] = pl.at(p, k) < pl.m ? v[p][k] - mean : 0.0f;
   }
-  float squares = 0.0f;
+  float even = 0.0f, odd = 0.0f;
 #pragma unroll
   for (int p = 0; p < P; ++p)
 #pragma unroll
-    for (int k = 0; k < kPiece; ++k) squares = fmaf(v[p][k], v[p][k], squares);
-  const float inv = rsqrtf(fmaf(row_sum<kWarp>(squares, sh, slot + 1), per, eps));
+    for (int k = 0; k < kPiece; k += 2) fma_two(even, odd, v[p][k], v[p][k + 1], v[p][k], v[p][k + 1], even, odd);
+  const float inv = rsqrtf(fmaf(row_sum<kWarp>(even + odd, sh, slot + 1), per, eps));
 #pragma unroll
   for (int p = 0; p < P; ++p)
 #pragma unroll
-    for (int k = 0; k < kPiece; ++k) v[p][k] *= inv;
+    for (int k = 0; k < kPiece; k += 2) mul_two(v[p][k], v[p][k + 1], v[p][k], v[p][k + 1], inv, inv);
 }
-// v = f(v, the row at w)
+// v = f(v, the row at w), two at a time
 template <int P, bool kVec, class F>
 __device__ __forceinline__ void with_row(const RowPlace<kVec>& pl, float (&v)[P][kPiece], const void* w, int dt, F f) {
   for_row<P, kVec>(pl, w, dt, [&](int p, const float (&u)[kPiece]) {
 #pragma unroll
-    for (int k = 0; k < kPiece; ++k) v[p][k] = f(v[p][k], u[k]);
+    for (int k = 0; k < kPiece; k += 2) f(v[p][k], v[p][k + 1], u[k], u[k + 1]);
   });
 }
 template <int P, bool kVec, bool kWarp, bool kAsync>
@@ -649,8 +669,9 @@ block_norm_kernel(const __grid_constant__ stb_norm a) {
         if (resid) load_row<P, kVec>(pl, row_of(resid, row, a.ldr, a.rdt), a.rdt, r);
       }
     }
-    auto times = [](float u, float f) { return u * f; };
-    auto plus = [](float u, float f) { return u + f; };
+    auto times = [](float& v0, float& v1, float f0, float f1) { mul_two(v0, v1, v0, v1, f0, f1); };
+    auto plus = [](float& v0, float& v1, float f0, float f1) { add_two(v0, v1, v0, v1, f0, f1); };
+    auto onto = [&](float& v0, float& v1, float r0, float r1) { fma_two(v0, v1, v0, v1, a.alpha, a.alpha, r0, r1); };
     if (a.post) {
       norm_row<P, kVec, kWarp>(pl, v, a.kind, a.eps, sh, slot);
       if (pw) with_row<P, kVec>(pl, v, pw, a.wdt, times);
@@ -666,14 +687,14 @@ block_norm_kernel(const __grid_constant__ stb_norm a) {
 #pragma unroll
       for (int p = 0; p < P; ++p)
 #pragma unroll
-        for (int k = 0; k < kPiece; ++k) v[p][k] = fmaf(a.alpha, v[p][k], r[p][k]);
+        for (int k = 0; k < kPiece; k += 2) onto(v[p][k], v[p][k + 1], r[p][k], r[p][k + 1]);
     } else if constexpr (kAsync) {
       for_slots<P>(pl, a.rdt, slot_r, [&](int p, const float (&u)[kPiece]) {
 #pragma unroll
-        for (int k = 0; k < kPiece; ++k) v[p][k] = fmaf(a.alpha, v[p][k], u[k]);
+        for (int k = 0; k < kPiece; k += 2) onto(v[p][k], v[p][k + 1], u[k], u[k + 1]);
       });
     } else {
-      with_row<P, kVec>(pl, v, row_of(resid, row, a.ldr, a.rdt), a.rdt, [&](float u, float f) { return fmaf(a.alpha, u, f); });
+      with_row<P, kVec>(pl, v, row_of(resid, row, a.ldr, a.rdt), a.rdt, onto);
     }
     if (a.resid_out) store_row<P, kVec>(pl, const_cast<char*>(row_of(a.resid_out, row, a.ldro, a.rdt)), a.rdt, v);
     const bool more = kAsync && row + stride < a.tokens;
