@@ -47,11 +47,14 @@ struct RowPlace {
   int lane, width, m;
   __device__ __forceinline__ int at(int p, int k) const { return kVec ? (p * width + lane) * kPiece + k : (p * kPiece + k) * width + lane; }
 };
-// The element types are arguments of the calls and template arguments of what runs per value: by_type chooses once per row.
+// The element types are arguments of the calls and template arguments of what runs per value: by_type chooses once per row, or, kAll, when the
+// kernel is compiled: one 16-bit type for everything is the usual call.
 template <int kType> struct TypeOf { static constexpr int value = kType; };
-template <class F>
+constexpr int kAnyType = -1;
+template <int kAll, class F>
 __device__ __forceinline__ void by_type(int dt, F f) {
-  if (dt == STB_F32) f(TypeOf<STB_F32>{});
+  if constexpr (kAll != kAnyType) f(TypeOf<kAll>{});
+  else if (dt == STB_F32) f(TypeOf<STB_F32>{});
   else if (dt == STB_F16) f(TypeOf<STB_F16>{});
   else f(TypeOf<STB_BF16>{});
 }
@@ -127,9 +130,9 @@ __device__ __forceinline__ RawPiece<kType> load_piece(const RowPlace<kVec>& pl, 
   return r;
 }
 // f(p, values) for every piece of the row at `row`, after all of its loads have been asked for.
-template <int P, bool kVec, class F>
+template <int kAll, int P, bool kVec, class F>
 __device__ __forceinline__ void for_row(const RowPlace<kVec>& pl, const void* row, int dt, F f) {
-  by_type(dt, [&](auto type) {
+  by_type<kAll>(dt, [&](auto type) {
     constexpr int kType = decltype(type)::value;
     constexpr int kAtOnce = kType == STB_F32 && P > 2 ? 2 : P;      // (registers)
 #pragma unroll
@@ -146,9 +149,9 @@ __device__ __forceinline__ void for_row(const RowPlace<kVec>& pl, const void* ro
     }
   });
 }
-template <int P, bool kVec>
+template <int kAll, int P, bool kVec>
 __device__ __forceinline__ void load_row(const RowPlace<kVec>& pl, const void* row, int dt, float (&v)[P][kPiece]) {
-  by_type(dt, [&](auto type) {
+  by_type<kAll>(dt, [&](auto type) {
     constexpr int kType = decltype(type)::value;
     RawPiece<kType> raw[P];
 #pragma unroll
@@ -157,9 +160,9 @@ __device__ __forceinline__ void load_row(const RowPlace<kVec>& pl, const void* r
     for (int p = 0; p < P; ++p) values_of<kType>(raw[p], v[p]);
   });
 }
-template <int P, bool kVec>
+template <int kAll, int P, bool kVec>
 __device__ __forceinline__ void store_row(const RowPlace<kVec>& pl, void* row, int dt, const float (&v)[P][kPiece]) {
-  by_type(dt, [&](auto type) {
+  by_type<kAll>(dt, [&](auto type) {
     constexpr int kType = decltype(type)::value;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
@@ -198,9 +201,9 @@ __device__ __forceinline__ void copy_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void copy_async_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-template <int P>
+template <int kAll, int P>
 __device__ __forceinline__ void ask_row(const RowPlace<true>& pl, const void* row, int dt, uint32_t slots) {
-  const int parts = dt == STB_F32 ? 2 : 1;
+  const int parts = (kAll == kAnyType ? dt : kAll) == STB_F32 ? 2 : 1;
 #pragma unroll
   for (int p = 0; p < P; ++p) {
     const int i = pl.at(p, 0);
@@ -226,9 +229,9 @@ __device__ __forceinline__ RawPiece<kType> slot_raw(const RowPlace<true>& pl, in
   return r;
 }
 // f(p, values) for every piece in the slots
-template <int P, class F>
+template <int kAll, int P, class F>
 __device__ __forceinline__ void for_slots(const RowPlace<true>& pl, int dt, uint32_t slots, F f) {
-  by_type(dt, [&](auto type) {
+  by_type<kAll>(dt, [&](auto type) {
     constexpr int kType = decltype(type)::value;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
@@ -266,14 +269,27 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v, float (*part)[32], int s
   v = lane < (int)(blockDim.x >> 5) ? __float_as_uint(part[slot][lane]) : 0u;
   return __reduce_max_sync(0xFFFFFFFFu, v);
 }
+// the largest of three, and of three a NaN if one is; the smallest of three
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  asm("max.f32 %0, %0, %1, %2;" : "+f"(a) : "f"(b), "f"(c));
+  return a;
+}
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(a) : "f"(b), "f"(c));
+  return a;
+}
+__device__ __forceinline__ float min3(float a, float b, float c) {
+  asm("min.f32 %0, %0, %1, %2;" : "+f"(a) : "f"(b), "f"(c));
+  return a;
+}
 template <int P>
 __device__ __forceinline__ uint32_t max_bits(const float (&v)[P][kPiece]) {
-  uint32_t b = 0;
+  float b = 0.0f;
 #pragma unroll
   for (int p = 0; p < P; ++p)
 #pragma unroll
-    for (int k = 0; k < kPiece; ++k) b = max(b, __float_as_uint(v[p][k]) & 0x7FFFFFFFu);
-  return b;
+    for (int k = 0; k < kPiece; k += 2) b = max3_nan(b, fabsf(v[p][k]), fabsf(v[p][k + 1]));
+  return __float_as_uint(b);
 }
 
 // ---- a row in 8 bits --------------------------------------------------------------------------------------------------------------
@@ -315,7 +331,7 @@ __device__ __forceinline__ void store_piece_i8(const RowPlace<kVec>& pl, int8_t*
     fma_two(u0, u1, v[k], v[k + 1], s.inverse, s.inverse, kRoundBias, kRoundBias);
     add_two(r0, r1, u0, u1, -kRoundBias, -kRoundBias);
     fma_two(d0, d1, v[k], v[k + 1], -s.inverse, -s.inverse, r0, r1);
-    off = fmaxf(off, fmaxf(fabsf(d0), fabsf(d1)));
+    off = max3(off, fabsf(d0), fabsf(d1));
     q[k] = __float_as_uint(u0);
     q[k + 1] = __float_as_uint(u1);
   }
@@ -429,7 +445,8 @@ __device__ __forceinline__ void gate_piece(QuantRow<P, kType>& r, int p, const u
   uint32_t lo[kPiece / 2], hi[kPiece / 2];
   float least = a[0];
 #pragma unroll
-  for (int k = 1; k < kPiece; ++k) least = fminf(least, a[k]);
+  for (int k = 1; k + 1 < kPiece; k += 2) least = min3(least, a[k], a[k + 1]);
+  least = fminf(least, a[kPiece - 1]);
 #pragma unroll
   for (int k = 0; k < kPiece / 2; ++k) gated_two<kType>(a[2 * k], a[2 * k + 1], b[2 * k], b[2 * k + 1], lo[k], hi[k]);
   if (least < -80.0f) {
@@ -468,8 +485,8 @@ quantize_i8_kernel(const QuantI8Args args) {
   auto row_x2 = [&](int r) { return static_cast<const char*>(x2) + (size_t)r * args.ldx2 * kBytes; };
   auto ask = [&](int r) {
     if constexpr (kAsync) {
-      ask_row<P>(pl, row_x(r), kType, slot_x);
-      if (kGated) ask_row<P>(pl, row_x2(r), kType, slot_x2);
+      ask_row<kType, P>(pl, row_x(r), kType, slot_x);
+      if (kGated) ask_row<kType, P>(pl, row_x2(r), kType, slot_x2);
     }
   };
   auto settle = [&](QuantRow<P, kType>& r, int p, float inverse, float largest) {
@@ -628,14 +645,15 @@ __device__ __forceinline__ void norm_row(const RowPlace<kVec>& pl, float (&v)[P]
     for (int k = 0; k < kPiece; k += 2) mul_two(v[p][k], v[p][k + 1], v[p][k], v[p][k + 1], inv, inv);
 }
 // v = f(v, the row at w), two at a time
-template <int P, bool kVec, class F>
+template <int kAll, int P, bool kVec, class F>
 __device__ __forceinline__ void with_row(const RowPlace<kVec>& pl, float (&v)[P][kPiece], const void* w, int dt, F f) {
-  for_row<P, kVec>(pl, w, dt, [&](int p, const float (&u)[kPiece]) {
+  for_row<kAll, P, kVec>(pl, w, dt, [&](int p, const float (&u)[kPiece]) {
 #pragma unroll
     for (int k = 0; k < kPiece; k += 2) f(v[p][k], v[p][k + 1], u[k], u[k + 1]);
   });
 }
-template <int P, bool kVec, bool kWarp, bool kAsync>
+// kAll: the type of x, the residual and the weights, where it is the same 16-bit type.
+template <int kAll, int P, bool kVec, bool kWarp, bool kAsync>
 __global__ void __launch_bounds__(kWarp ? 256 : (kAsync ? 512 : kMaxRowThreads), kWarp || (kAsync && P <= 4) ? 2 : 1)
 block_norm_kernel(const __grid_constant__ stb_norm a) {
   extern __shared__ __align__(16) uint8_t slots[];
@@ -646,11 +664,11 @@ block_norm_kernel(const __grid_constant__ stb_norm a) {
   int row = kWarp ? (int)(blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5)) : (int)blockIdx.x, slot = 0;
   const RowPlace<kVec> pl{kWarp ? (int)(threadIdx.x & 31) : (int)threadIdx.x, kWarp ? 32 : (int)blockDim.x, a.h};
   auto row_of = [&](const void* base, size_t r, size_t ld, int dt) { return static_cast<const char*>(base) + r * ld * (size_t)dtype_bytes(dt); };
-  const uint32_t slot_x = kAsync ? smem_u32(slots) : 0u, slot_r = slot_x + (uint32_t)(P * pl.width) * 16u * (a.xdt == STB_F32 ? 2u : 1u);
+  const uint32_t slot_x = kAsync ? smem_u32(slots) : 0u, slot_r = slot_x + (uint32_t)(P * pl.width) * 16u * ((kAll == kAnyType ? a.xdt : kAll) == STB_F32 ? 2u : 1u);
   auto ask = [&](int r) {
     if constexpr (kAsync) {
-      ask_row<P>(pl, row_of(x, r, a.ldx, a.xdt), a.xdt, slot_x);
-      if (resid) ask_row<P>(pl, row_of(resid, r, a.ldr, a.rdt), a.rdt, slot_r);
+      ask_row<kAll, P>(pl, row_of(x, r, a.ldx, a.xdt), a.xdt, slot_x);
+      if (resid) ask_row<kAll, P>(pl, row_of(resid, r, a.ldr, a.rdt), a.rdt, slot_r);
     }
   };
   if (kAsync && row < a.tokens) ask(row);
@@ -659,14 +677,14 @@ block_norm_kernel(const __grid_constant__ stb_norm a) {
     float v[P][kPiece], r[kEarly ? P : 1][kPiece];
     if constexpr (kAsync) {
       copy_async_done();
-      for_slots<P>(pl, a.xdt, slot_x, [&](int p, const float (&u)[kPiece]) {
+      for_slots<kAll, P>(pl, a.xdt, slot_x, [&](int p, const float (&u)[kPiece]) {
 #pragma unroll
         for (int k = 0; k < kPiece; ++k) v[p][k] = u[k];
       });
     } else {
-      load_row<P, kVec>(pl, row_of(x, row, a.ldx, a.xdt), a.xdt, v);
+      load_row<kAll, P, kVec>(pl, row_of(x, row, a.ldx, a.xdt), a.xdt, v);
       if constexpr (kEarly) {
-        if (resid) load_row<P, kVec>(pl, row_of(resid, row, a.ldr, a.rdt), a.rdt, r);
+        if (resid) load_row<kAll, P, kVec>(pl, row_of(resid, row, a.ldr, a.rdt), a.rdt, r);
       }
     }
     auto times = [](float& v0, float& v1, float f0, float f1) { mul_two(v0, v1, v0, v1, f0, f1); };
@@ -674,10 +692,10 @@ block_norm_kernel(const __grid_constant__ stb_norm a) {
     auto onto = [&](float& v0, float& v1, float r0, float r1) { fma_two(v0, v1, v0, v1, a.alpha, a.alpha, r0, r1); };
     if (a.post) {
       norm_row<P, kVec, kWarp>(pl, v, a.kind, a.eps, sh, slot);
-      if (pw) with_row<P, kVec>(pl, v, pw, a.wdt, times);
-      if (pb) with_row<P, kVec>(pl, v, pb, a.wdt, plus);
+      if (pw) with_row<kAll, P, kVec>(pl, v, pw, a.wdt, times);
+      if (pb) with_row<kAll, P, kVec>(pl, v, pb, a.wdt, plus);
     }
-    if (gate) with_row<P, kVec>(pl, v, row_of(gate, row / a.tokens_per_gate, a.ldgate, a.wdt), a.wdt, times);
+    if (gate) with_row<kAll, P, kVec>(pl, v, row_of(gate, row / a.tokens_per_gate, a.ldgate, a.wdt), a.wdt, times);
     if (!resid) {
 #pragma unroll
       for (int p = 0; p < P; ++p)
@@ -689,14 +707,14 @@ block_norm_kernel(const __grid_constant__ stb_norm a) {
 #pragma unroll
         for (int k = 0; k < kPiece; k += 2) onto(v[p][k], v[p][k + 1], r[p][k], r[p][k + 1]);
     } else if constexpr (kAsync) {
-      for_slots<P>(pl, a.rdt, slot_r, [&](int p, const float (&u)[kPiece]) {
+      for_slots<kAll, P>(pl, a.rdt, slot_r, [&](int p, const float (&u)[kPiece]) {
 #pragma unroll
         for (int k = 0; k < kPiece; k += 2) onto(v[p][k], v[p][k + 1], u[k], u[k + 1]);
       });
     } else {
-      with_row<P, kVec>(pl, v, row_of(resid, row, a.ldr, a.rdt), a.rdt, onto);
+      with_row<kAll, P, kVec>(pl, v, row_of(resid, row, a.ldr, a.rdt), a.rdt, onto);
     }
-    if (a.resid_out) store_row<P, kVec>(pl, const_cast<char*>(row_of(a.resid_out, row, a.ldro, a.rdt)), a.rdt, v);
+    if (a.resid_out) store_row<kAll, P, kVec>(pl, const_cast<char*>(row_of(a.resid_out, row, a.ldro, a.rdt)), a.rdt, v);
     const bool more = kAsync && row + stride < a.tokens;
     if (!a.y && !a.q) {
       if (more) ask(row + stride);
@@ -704,9 +722,9 @@ block_norm_kernel(const __grid_constant__ stb_norm a) {
     }
     norm_row<P, kVec, kWarp>(pl, v, a.kind, a.eps, sh, slot + 2);
     if (more) ask(row + stride);                   // (this row's pieces have been read: its sum is known)
-    if (w) with_row<P, kVec>(pl, v, w, a.wdt, times);
-    if (b) with_row<P, kVec>(pl, v, b, a.wdt, plus);
-    if (a.y) store_row<P, kVec>(pl, const_cast<char*>(row_of(a.y, row, a.ldy, a.ydt)), a.ydt, v);
+    if (w) with_row<kAll, P, kVec>(pl, v, w, a.wdt, times);
+    if (b) with_row<kAll, P, kVec>(pl, v, b, a.wdt, plus);
+    if (a.y) store_row<kAnyType, P, kVec>(pl, const_cast<char*>(row_of(a.y, row, a.ldy, a.ydt)), a.ydt, v);
     if (a.q) {
       const RowScale s = row_scale(row_max<kWarp>(max_bits<P>(v), sh, slot + 4));
       if (pl.lane == 0) a.q_scale[row] = s.scale;
@@ -799,6 +817,21 @@ static cudaError_t launch_quantize(const QuantI8Args& a, const RowShape& s, bool
   }
 }
 
+template <int kAll>
+static cudaError_t launch_norm(const stb_norm& a, const RowShape& s, bool vec, cudaStream_t st) {
+  switch (s.form) {
+    case kRowWarp:
+      if (s.pieces == 1) return vec ? launch_rows<block_norm_kernel<kAll, 1, true, true, false>>(s, st, a) : launch_rows<block_norm_kernel<kAll, 1, false, true, false>>(s, st, a);
+      return vec ? launch_rows<block_norm_kernel<kAll, 4, true, true, false>>(s, st, a) : launch_rows<block_norm_kernel<kAll, 4, false, true, false>>(s, st, a);
+    case kRowAsync:
+      return s.pieces == 4 ? launch_rows<block_norm_kernel<kAll, 4, true, false, true>>(s, st, a) : launch_rows<block_norm_kernel<kAll, 8, true, false, true>>(s, st, a);
+    default:
+      if (s.pieces == 1) return vec ? launch_rows<block_norm_kernel<kAll, 1, true, false, false>>(s, st, a) : launch_rows<block_norm_kernel<kAll, 1, false, false, false>>(s, st, a);
+      if (s.pieces == 2) return vec ? launch_rows<block_norm_kernel<kAll, 2, true, false, false>>(s, st, a) : launch_rows<block_norm_kernel<kAll, 2, false, false, false>>(s, st, a);
+      return vec ? launch_rows<block_norm_kernel<kAll, 4, true, false, false>>(s, st, a) : launch_rows<block_norm_kernel<kAll, 4, false, false, false>>(s, st, a);
+  }
+}
+
 }  // namespace stb
 
 extern "C" int stb_quantize_i8(const void* x, size_t ldx, const void* x2, size_t ldx2, stb_dtype xdt, int rows, int m, int8_t* q, size_t ldq,
@@ -819,8 +852,6 @@ extern "C" int stb_quantize_i8(const void* x, size_t ldx, const void* x2, size_t
                                              : (half ? stb::launch_quantize<STB_F16, false>(a, s, vec, st) : stb::launch_quantize<STB_BF16, false>(a, s, vec, st)));
   return e == cudaSuccess ? STB_OK : STB_ERR_CUDA;
 }
-
-static int status(cudaError_t e) { return e == cudaSuccess ? STB_OK : STB_ERR_CUDA; }
 
 extern "C" int stb_block_norm(const stb_norm* args, void* stream) {
   if (!args) return STB_ERR_ARG;
@@ -850,15 +881,7 @@ extern "C" int stb_block_norm(const stb_norm* args, void* stream) {
   const uint32_t slot = (a.xdt == STB_F32 ? 32u : 16u) + (!a.resid ? 0u : (a.rdt == STB_F32 ? 32u : 16u));
   const stb::RowShape s = stb::row_shape(a.h, a.tokens, vec, slot, 10u * 128u, 1024, 512);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  switch (s.form) {
-    case stb::kRowWarp:
-      if (s.pieces == 1) return vec ? status(stb::launch_rows<stb::block_norm_kernel<1, true, true, false>>(s, st, a)) : status(stb::launch_rows<stb::block_norm_kernel<1, false, true, false>>(s, st, a));
-      return vec ? status(stb::launch_rows<stb::block_norm_kernel<4, true, true, false>>(s, st, a)) : status(stb::launch_rows<stb::block_norm_kernel<4, false, true, false>>(s, st, a));
-    case stb::kRowAsync:
-      return s.pieces == 4 ? status(stb::launch_rows<stb::block_norm_kernel<4, true, false, true>>(s, st, a)) : status(stb::launch_rows<stb::block_norm_kernel<8, true, false, true>>(s, st, a));
-    default:
-      if (s.pieces == 1) return vec ? status(stb::launch_rows<stb::block_norm_kernel<1, true, false, false>>(s, st, a)) : status(stb::launch_rows<stb::block_norm_kernel<1, false, false, false>>(s, st, a));
-      if (s.pieces == 2) return vec ? status(stb::launch_rows<stb::block_norm_kernel<2, true, false, false>>(s, st, a)) : status(stb::launch_rows<stb::block_norm_kernel<2, false, false, false>>(s, st, a));
-      return vec ? status(stb::launch_rows<stb::block_norm_kernel<4, true, false, false>>(s, st, a)) : status(stb::launch_rows<stb::block_norm_kernel<4, false, false, false>>(s, st, a));
-  }
+  const bool same = a.xdt != STB_F32 && (!residual || a.rdt == a.xdt) && (!vectors || a.wdt == a.xdt);
+  const cudaError_t e = !same ? stb::launch_norm<stb::kAnyType>(a, s, vec, st) : (a.xdt == STB_F16 ? stb::launch_norm<STB_F16>(a, s, vec, st) : stb::launch_norm<STB_BF16>(a, s, vec, st));
+  return e == cudaSuccess ? STB_OK : STB_ERR_CUDA;
 }
