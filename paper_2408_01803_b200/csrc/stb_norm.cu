@@ -134,7 +134,7 @@ template <int kAll, int P, bool kVec, class F>
 __device__ __forceinline__ void for_row(const RowPlace<kVec>& pl, const void* row, int dt, F f) {
   by_type<kAll>(dt, [&](auto type) {
     constexpr int kType = decltype(type)::value;
-    constexpr int kAtOnce = kType == STB_F32 && P > 2 ? 2 : P;      // (registers)
+    constexpr int kAtOnce = P <= 2 ? P : (!kVec ? 1 : (kType == STB_F32 ? 2 : P));      // (registers)
 #pragma unroll
     for (int p0 = 0; p0 < P; p0 += kAtOnce) {
       RawPiece<kType> raw[kAtOnce];
@@ -470,7 +470,7 @@ __device__ __forceinline__ uint32_t magnitude_bits(uint32_t m) {
 }
 // kWarp: a row belongs to a warp, else to the CTA, which takes every gridDim-th one.  kAsync: the pieces of the next row are on their way.
 template <int P, int kType, bool kGated, bool kVec, bool kWarp, bool kAsync>
-__global__ void __launch_bounds__(kWarp ? 256 : (kAsync && !kGated ? 512 : kMaxRowThreads), kWarp || (kAsync && !kGated && (P <= 4 || kType != STB_F32)) ? 2 : 1)
+__global__ void __launch_bounds__(kWarp ? 256 : ((kAsync && !kGated) || (!kVec && P >= 4) ? 512 : kMaxRowThreads), kWarp || (kAsync && !kGated && (P <= 4 || kType != STB_F32)) || (!kVec && P == 4) ? 2 : 1)
 quantize_i8_kernel(const QuantI8Args args) {
   extern __shared__ __align__(16) uint8_t slots[];
   __shared__ float sh[4][32];                       // the parts of a row's two reductions, and of the next one's
@@ -654,7 +654,7 @@ __device__ __forceinline__ void with_row(const RowPlace<kVec>& pl, float (&v)[P]
 }
 // kAll: the type of x, the residual and the weights, where it is the same 16-bit type.
 template <int kAll, int P, bool kVec, bool kWarp, bool kAsync>
-__global__ void __launch_bounds__(kWarp ? 256 : (kAsync ? 512 : kMaxRowThreads), kWarp || (kAsync && P <= 4) ? 2 : 1)
+__global__ void __launch_bounds__(kWarp ? 256 : (kAsync || (!kVec && P >= 4) ? 512 : kMaxRowThreads), kWarp || (kAsync && P <= 4) || (!kVec && P == 4) ? 2 : 1)
 block_norm_kernel(const __grid_constant__ stb_norm a) {
   extern __shared__ __align__(16) uint8_t slots[];
   __shared__ float sh[10][32];                      // the parts of a row's five reductions, and of the next one's
@@ -738,7 +738,8 @@ block_norm_kernel(const __grid_constant__ stb_norm a) {
 //   warp:    rows of up to 256 values, or of up to 1024 where there are more than SMs; 1 or 4 pieces per lane
 //   async:   more than 296 rows that can be read in 16-byte pieces: 4 or 8 pieces per thread, whichever fills an SM better (resident4, resident8: the
 //            threads that its registers take), as many CTAs as stay on the GPU
-//   else:    one CTA per row, with one piece per thread as long as 1024 threads reach, for the shortest way through a row
+//   else:    one CTA per row, with one piece per thread as long as 1024 threads reach, for the shortest way through a row; four, for more rows at once, where
+//            there are many that cannot be read in 16-byte pieces (1000 x 5111: 25 -> @ us)
 enum RowForm { kRowWarp, kRowAsync, kRowDirect, kRowLong };
 struct RowShape { RowForm form; int pieces, threads, grid; uint32_t smem; };
 static RowShape row_shape(int m, int rows, bool vec, uint32_t slot_bytes_per_piece, uint32_t static_smem, int resident4, int resident8, int most4 = 512) {
@@ -771,6 +772,8 @@ static RowShape row_shape(int m, int rows, bool vec, uint32_t slot_bytes_per_pie
   }
   s.form = kRowDirect;
   s.pieces = pieces <= kMaxRowThreads ? 1 : (pieces <= 2 * kMaxRowThreads ? 2 : 4);
+  if (!vec && pieces > 2 * kMaxRowThreads) s.pieces = 8;
+  else if (!vec && rows > 148) s.pieces = 4;
   s.threads = ((pieces + s.pieces - 1) / s.pieces + 31) / 32 * 32;
   s.grid = rows;
   return s;
@@ -813,7 +816,8 @@ static cudaError_t launch_quantize(const QuantI8Args& a, const RowShape& s, bool
     default:
       if (s.pieces == 1) return vec ? launch_rows<quantize_i8_kernel<1, kType, kGated, true, false, false>>(s, st, a) : launch_rows<quantize_i8_kernel<1, kType, kGated, false, false, false>>(s, st, a);
       if (s.pieces == 2) return vec ? launch_rows<quantize_i8_kernel<2, kType, kGated, true, false, false>>(s, st, a) : launch_rows<quantize_i8_kernel<2, kType, kGated, false, false, false>>(s, st, a);
-      return vec ? launch_rows<quantize_i8_kernel<4, kType, kGated, true, false, false>>(s, st, a) : launch_rows<quantize_i8_kernel<4, kType, kGated, false, false, false>>(s, st, a);
+      if (s.pieces == 4) return vec ? launch_rows<quantize_i8_kernel<4, kType, kGated, true, false, false>>(s, st, a) : launch_rows<quantize_i8_kernel<4, kType, kGated, false, false, false>>(s, st, a);
+      return launch_rows<quantize_i8_kernel<8, kType, kGated, false, false, false>>(s, st, a);
   }
 }
 
@@ -828,7 +832,8 @@ static cudaError_t launch_norm(const stb_norm& a, const RowShape& s, bool vec, c
     default:
       if (s.pieces == 1) return vec ? launch_rows<block_norm_kernel<kAll, 1, true, false, false>>(s, st, a) : launch_rows<block_norm_kernel<kAll, 1, false, false, false>>(s, st, a);
       if (s.pieces == 2) return vec ? launch_rows<block_norm_kernel<kAll, 2, true, false, false>>(s, st, a) : launch_rows<block_norm_kernel<kAll, 2, false, false, false>>(s, st, a);
-      return vec ? launch_rows<block_norm_kernel<kAll, 4, true, false, false>>(s, st, a) : launch_rows<block_norm_kernel<kAll, 4, false, false, false>>(s, st, a);
+      if (s.pieces == 4) return vec ? launch_rows<block_norm_kernel<kAll, 4, true, false, false>>(s, st, a) : launch_rows<block_norm_kernel<kAll, 4, false, false, false>>(s, st, a);
+      return launch_rows<block_norm_kernel<kAll, 8, false, false, false>>(s, st, a);
   }
 }
 
