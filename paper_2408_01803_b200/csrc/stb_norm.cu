@@ -134,7 +134,7 @@ template <int kAll, int P, bool kVec, class F>
 __device__ __forceinline__ void for_row(const RowPlace<kVec>& pl, const void* row, int dt, F f) {
   by_type<kAll>(dt, [&](auto type) {
     constexpr int kType = decltype(type)::value;
-    constexpr int kAtOnce = P <= 2 ? P : (!kVec ? 1 : (kType == STB_F32 ? 2 : P));      // (registers)
+    constexpr int kAtOnce = P <= 2 ? P : (!kVec || kType == STB_F32 ? 2 : P);      // (registers)
 #pragma unroll
     for (int p0 = 0; p0 < P; p0 += kAtOnce) {
       RawPiece<kType> raw[kAtOnce];
@@ -202,7 +202,8 @@ __device__ __forceinline__ void copy_async16(uint32_t dst, const void* src) {
 }
 __device__ __forceinline__ void copy_async_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 template <int kAll, int P>
-__device__ __forceinline__ void ask_row(const RowPlace<true>& pl, const void* row, int dt, uint32_t slots) {
+__device__ __forceinline__ void ask_row(const RowPlace<true>& pl, const void* row, int dt, uint8_t* at) {
+  const uint32_t slots = smem_u32(at);
   const int parts = (kAll == kAnyType ? dt : kAll) == STB_F32 ? 2 : 1;
 #pragma unroll
   for (int p = 0; p < P; ++p) {
@@ -214,23 +215,21 @@ __device__ __forceinline__ void ask_row(const RowPlace<true>& pl, const void* ro
     if (parts == 2) copy_async16(dst + (uint32_t)pl.width * 16u, src + 16);
   }
 }
-__device__ __forceinline__ uint4 slot_piece(uint32_t a) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
-  return v;
-}
 template <int kType>
-__device__ __forceinline__ RawPiece<kType> slot_raw(const RowPlace<true>& pl, int p, uint32_t slots) {
+__device__ __forceinline__ RawPiece<kType> slot_raw(const RowPlace<true>& pl, int p, const uint8_t* slots) {
   constexpr int kParts = kType == STB_F32 ? 2 : 1;
   RawPiece<kType> r;
 #pragma unroll
-  for (int h = 0; h < kParts; ++h)
-    r.w[h] = pl.at(p, 0) < pl.m ? slot_piece(slots + (uint32_t)((kParts * p + h) * pl.width + pl.lane) * 16u) : make_uint4(0u, 0u, 0u, 0u);
+  for (int h = 0; h < kParts; ++h) {
+    const uint4 v = reinterpret_cast<const uint4*>(slots)[(kParts * p + h) * pl.width + pl.lane];      // (behind the row's end: whatever is there)
+    const bool in = pl.at(p, 0) < pl.m;
+    r.w[h] = make_uint4(in ? v.x : 0u, in ? v.y : 0u, in ? v.z : 0u, in ? v.w : 0u);
+  }
   return r;
 }
 // f(p, values) for every piece in the slots
 template <int kAll, int P, class F>
-__device__ __forceinline__ void for_slots(const RowPlace<true>& pl, int dt, uint32_t slots, F f) {
+__device__ __forceinline__ void for_slots(const RowPlace<true>& pl, int dt, const uint8_t* slots, F f) {
   by_type<kAll>(dt, [&](auto type) {
     constexpr int kType = decltype(type)::value;
 #pragma unroll
@@ -470,7 +469,8 @@ __device__ __forceinline__ uint32_t magnitude_bits(uint32_t m) {
 }
 // kWarp: a row belongs to a warp, else to the CTA, which takes every gridDim-th one.  kAsync: the pieces of the next row are on their way.
 template <int P, int kType, bool kGated, bool kVec, bool kWarp, bool kAsync>
-__global__ void __launch_bounds__(kWarp ? 256 : ((kAsync && !kGated) || (!kVec && P >= 4) ? 512 : kMaxRowThreads), kWarp || (kAsync && !kGated && (P <= 4 || kType != STB_F32)) || (!kVec && P == 4) ? 2 : 1)
+__global__ void __launch_bounds__(kWarp ? 256 : (kAsync ? (kGated ? kMaxRowThreads : 512) : (!kVec && P > 2 ? 512 : kMaxRowThreads)),
+                                  kWarp || (kAsync && !kGated && (P <= 4 || kType != STB_F32)) || (!kVec && P == 4) ? 2 : 1)
 quantize_i8_kernel(const QuantI8Args args) {
   extern __shared__ __align__(16) uint8_t slots[];
   __shared__ float sh[4][32];                       // the parts of a row's two reductions, and of the next one's
@@ -480,7 +480,7 @@ quantize_i8_kernel(const QuantI8Args args) {
   const int stride = kWarp ? (int)(gridDim.x * (blockDim.x >> 5)) : (int)gridDim.x;
   int row = kWarp ? (int)(blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5)) : (int)blockIdx.x, slot = 0;
   const RowPlace<kVec> pl{kWarp ? (int)(threadIdx.x & 31) : (int)threadIdx.x, kWarp ? 32 : (int)blockDim.x, args.m};
-  const uint32_t slot_x = kAsync ? smem_u32(slots) : 0u, slot_x2 = slot_x + (uint32_t)(P * pl.width) * 16u;
+  uint8_t *slot_x = slots, *slot_x2 = slots + (size_t)(P * pl.width) * 16u;
   auto row_x = [&](int r) { return static_cast<const char*>(x) + (size_t)r * args.ldx * kBytes; };
   auto row_x2 = [&](int r) { return static_cast<const char*>(x2) + (size_t)r * args.ldx2 * kBytes; };
   auto ask = [&](int r) {
@@ -654,7 +654,7 @@ __device__ __forceinline__ void with_row(const RowPlace<kVec>& pl, float (&v)[P]
 }
 // kAll: the type of x, the residual and the weights, where it is the same 16-bit type.
 template <int kAll, int P, bool kVec, bool kWarp, bool kAsync>
-__global__ void __launch_bounds__(kWarp ? 256 : (kAsync || (!kVec && P >= 4) ? 512 : kMaxRowThreads), kWarp || (kAsync && P <= 4) || (!kVec && P == 4) ? 2 : 1)
+__global__ void __launch_bounds__(kWarp ? 256 : (kAsync || (!kVec && P > 2) ? 512 : kMaxRowThreads), kWarp || (kAsync && P <= 4) ? 2 : 1)
 block_norm_kernel(const __grid_constant__ stb_norm a) {
   extern __shared__ __align__(16) uint8_t slots[];
   __shared__ float sh[10][32];                      // the parts of a row's five reductions, and of the next one's
@@ -664,7 +664,7 @@ block_norm_kernel(const __grid_constant__ stb_norm a) {
   int row = kWarp ? (int)(blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5)) : (int)blockIdx.x, slot = 0;
   const RowPlace<kVec> pl{kWarp ? (int)(threadIdx.x & 31) : (int)threadIdx.x, kWarp ? 32 : (int)blockDim.x, a.h};
   auto row_of = [&](const void* base, size_t r, size_t ld, int dt) { return static_cast<const char*>(base) + r * ld * (size_t)dtype_bytes(dt); };
-  const uint32_t slot_x = kAsync ? smem_u32(slots) : 0u, slot_r = slot_x + (uint32_t)(P * pl.width) * 16u * ((kAll == kAnyType ? a.xdt : kAll) == STB_F32 ? 2u : 1u);
+  uint8_t *slot_x = slots, *slot_r = slots + (size_t)(P * pl.width) * ((kAll == kAnyType ? a.xdt : kAll) == STB_F32 ? 32u : 16u);
   auto ask = [&](int r) {
     if constexpr (kAsync) {
       ask_row<kAll, P>(pl, row_of(x, r, a.ldx, a.xdt), a.xdt, slot_x);
@@ -736,19 +736,19 @@ block_norm_kernel(const __grid_constant__ stb_norm a) {
 // ---- launches -----------------------------------------------------------------------------------------------------------------------
 // How rows of m values are dealt out.
 //   warp:    rows of up to 256 values, or of up to 1024 where there are more than SMs; 1 or 4 pieces per lane
-//   async:   more than 296 rows that can be read in 16-byte pieces: 4 or 8 pieces per thread, whichever fills an SM better (resident4, resident8: the
-//            threads that its registers take), as many CTAs as stay on the GPU
-//   else:    one CTA per row, with one piece per thread as long as 1024 threads reach, for the shortest way through a row; four, for more rows at once, where
-//            there are many that cannot be read in 16-byte pieces (1000 x 5111: 25 -> @ us)
-enum RowForm { kRowWarp, kRowAsync, kRowDirect, kRowLong };
-struct RowShape { RowForm form; int pieces, threads, grid; uint32_t smem; };
-static RowShape row_shape(int m, int rows, bool vec, uint32_t slot_bytes_per_piece, uint32_t static_smem, int resident4, int resident8, int most4 = 512) {
+//   slots:   the next row on its way into shared memory: more than 296 rows that can be read in 16-byte pieces, 4 or 8 pieces per thread, whichever fills
+//            an SM better (resident4, resident8: the threads that its registers take; most4: a CTA's with 4), as many CTAs as stay on the GPU
+//   else:    one CTA per row, with one piece per thread as long as 1024 threads reach, for the shortest way through a row; `any_pieces` of them where there are
+//            many rows and no 16-byte pieces, for more rows at a time
+struct RowShape { bool warp, slots, longer; int pieces, threads, grid; uint32_t smem; };
+struct RowNeeds { uint32_t piece_bytes, static_smem; int resident4, resident8, most4, any_pieces; };
+static RowShape row_shape(int m, int rows, bool vec, const RowNeeds& need) {
   RowShape s = {};
   const int pieces = (m + kPiece - 1) / kPiece;
-  if (m > kMaxRow) { s.form = kRowLong; s.pieces = 1; s.threads = kMaxRowThreads; s.grid = rows; return s; }
+  if (m > kMaxRow) { s.longer = true; s.pieces = 1; s.threads = kMaxRowThreads; s.grid = rows; return s; }
   if (m <= 256 || (m <= 1024 && rows > 148)) {
     const int per_cta = rows >= 148 * 8 ? 8 : (rows >= 148 * 2 ? 2 : 1);
-    s.form = kRowWarp;
+    s.warp = true;
     s.pieces = pieces <= 32 ? 1 : 4;
     s.threads = 32 * per_cta;
     s.grid = (rows + per_cta - 1) / per_cta;
@@ -756,24 +756,22 @@ static RowShape row_shape(int m, int rows, bool vec, uint32_t slot_bytes_per_pie
   }
   if (vec && rows > 296) {
     const int threads4 = ((pieces + 3) / 4 + 31) / 32 * 32, threads8 = ((pieces + 7) / 8 + 31) / 32 * 32;
-    const bool four = threads4 <= most4 && resident4 / threads4 * threads4 >= resident8 / threads8 * threads8;      // threads that an SM holds
+    const bool four = threads4 <= need.most4 && need.resident4 / threads4 * threads4 >= need.resident8 / threads8 * threads8;      // threads that an SM holds
     s.pieces = four ? 4 : 8;
     s.threads = four ? threads4 : threads8;
-    s.smem = (uint32_t)(s.pieces * s.threads) * slot_bytes_per_piece;
+    s.smem = (uint32_t)(s.pieces * s.threads) * need.piece_bytes;
     if (s.smem <= (uint32_t)kMaxRowSmem) {          // (not two inputs of fp32 beyond 28672 values)
-      int resident = (four ? resident4 : resident8) / s.threads, by_smem = (int)(228u * 1024u / (s.smem + 1024u + static_smem));
+      int resident = (four ? need.resident4 : need.resident8) / s.threads, by_smem = (int)(228u * 1024u / (s.smem + 1024u + need.static_smem));
       if (resident > by_smem) resident = by_smem;
       if (resident < 1) resident = 1;
-      s.form = kRowAsync;
+      s.slots = true;
       s.grid = rows < 148 * resident ? rows : 148 * resident;
       return s;
     }
     s.smem = 0;
   }
-  s.form = kRowDirect;
-  s.pieces = pieces <= kMaxRowThreads ? 1 : (pieces <= 2 * kMaxRowThreads ? 2 : 4);
-  if (!vec && pieces > 2 * kMaxRowThreads) s.pieces = 8;
-  else if (!vec && rows > 148) s.pieces = 4;
+  s.pieces = pieces <= kMaxRowThreads ? 1 : (pieces <= 2 * kMaxRowThreads ? 2 : (vec ? 4 : 8));
+  if (!vec && rows > 148 && s.pieces < need.any_pieces) s.pieces = need.any_pieces;
   s.threads = ((pieces + s.pieces - 1) / s.pieces + 31) / 32 * 32;
   s.grid = rows;
   return s;
@@ -800,41 +798,39 @@ static cudaError_t launch_rows(const RowShape& s, cudaStream_t st, const A& args
   return launch_after(kKernel, dim3((unsigned)s.grid), dim3((unsigned)s.threads), s.smem, st, args);
 }
 
+template <int kType, bool kGated, bool kVec>
+static cudaError_t launch_quantize_as(const QuantI8Args& a, const RowShape& s, cudaStream_t st) {
+  if (s.longer) return launch_rows<quantize_i8_long_kernel<kType, kGated, kVec>>(s, st, a);
+  if (s.warp) return s.pieces == 1 ? launch_rows<quantize_i8_kernel<1, kType, kGated, kVec, true, false>>(s, st, a) : launch_rows<quantize_i8_kernel<4, kType, kGated, kVec, true, false>>(s, st, a);
+  if constexpr (kVec) {
+    if constexpr (!kGated) {
+      if (s.slots && s.pieces == 8) return launch_rows<quantize_i8_kernel<8, kType, kGated, true, false, true>>(s, st, a);
+    }
+    if (s.slots) return launch_rows<quantize_i8_kernel<4, kType, kGated, true, false, true>>(s, st, a);
+  } else if (s.pieces == 8) {
+    return launch_rows<quantize_i8_kernel<8, kType, kGated, false, false, false>>(s, st, a);
+  }
+  if (s.pieces == 1) return launch_rows<quantize_i8_kernel<1, kType, kGated, kVec, false, false>>(s, st, a);
+  if (s.pieces == 2) return launch_rows<quantize_i8_kernel<2, kType, kGated, kVec, false, false>>(s, st, a);
+  return launch_rows<quantize_i8_kernel<4, kType, kGated, kVec, false, false>>(s, st, a);
+}
 template <int kType, bool kGated>
 static cudaError_t launch_quantize(const QuantI8Args& a, const RowShape& s, bool vec, cudaStream_t st) {
-  switch (s.form) {
-    case kRowLong:
-      return vec ? launch_rows<quantize_i8_long_kernel<kType, kGated, true>>(s, st, a) : launch_rows<quantize_i8_long_kernel<kType, kGated, false>>(s, st, a);
-    case kRowWarp:
-      if (s.pieces == 1) return vec ? launch_rows<quantize_i8_kernel<1, kType, kGated, true, true, false>>(s, st, a) : launch_rows<quantize_i8_kernel<1, kType, kGated, false, true, false>>(s, st, a);
-      return vec ? launch_rows<quantize_i8_kernel<4, kType, kGated, true, true, false>>(s, st, a) : launch_rows<quantize_i8_kernel<4, kType, kGated, false, true, false>>(s, st, a);
-    case kRowAsync:
-      if constexpr (!kGated) {
-        if (s.pieces == 8) return launch_rows<quantize_i8_kernel<8, kType, kGated, true, false, true>>(s, st, a);
-      }
-      return launch_rows<quantize_i8_kernel<4, kType, kGated, true, false, true>>(s, st, a);
-    default:
-      if (s.pieces == 1) return vec ? launch_rows<quantize_i8_kernel<1, kType, kGated, true, false, false>>(s, st, a) : launch_rows<quantize_i8_kernel<1, kType, kGated, false, false, false>>(s, st, a);
-      if (s.pieces == 2) return vec ? launch_rows<quantize_i8_kernel<2, kType, kGated, true, false, false>>(s, st, a) : launch_rows<quantize_i8_kernel<2, kType, kGated, false, false, false>>(s, st, a);
-      if (s.pieces == 4) return vec ? launch_rows<quantize_i8_kernel<4, kType, kGated, true, false, false>>(s, st, a) : launch_rows<quantize_i8_kernel<4, kType, kGated, false, false, false>>(s, st, a);
-      return launch_rows<quantize_i8_kernel<8, kType, kGated, false, false, false>>(s, st, a);
-  }
+  return vec ? launch_quantize_as<kType, kGated, true>(a, s, st) : launch_quantize_as<kType, kGated, false>(a, s, st);
 }
-
+template <int kAll, bool kVec>
+static cudaError_t launch_norm_as(const stb_norm& a, const RowShape& s, cudaStream_t st) {
+  if (s.warp) return s.pieces == 1 ? launch_rows<block_norm_kernel<kAll, 1, kVec, true, false>>(s, st, a) : launch_rows<block_norm_kernel<kAll, 4, kVec, true, false>>(s, st, a);
+  if constexpr (kVec) {
+    if (s.slots) return s.pieces == 4 ? launch_rows<block_norm_kernel<kAll, 4, true, false, true>>(s, st, a) : launch_rows<block_norm_kernel<kAll, 8, true, false, true>>(s, st, a);
+  }
+  if (s.pieces == 1) return launch_rows<block_norm_kernel<kAll, 1, kVec, false, false>>(s, st, a);
+  if (s.pieces == 2) return launch_rows<block_norm_kernel<kAll, 2, kVec, false, false>>(s, st, a);
+  return launch_rows<block_norm_kernel<kAll, kVec ? 4 : 8, kVec, false, false>>(s, st, a);
+}
 template <int kAll>
 static cudaError_t launch_norm(const stb_norm& a, const RowShape& s, bool vec, cudaStream_t st) {
-  switch (s.form) {
-    case kRowWarp:
-      if (s.pieces == 1) return vec ? launch_rows<block_norm_kernel<kAll, 1, true, true, false>>(s, st, a) : launch_rows<block_norm_kernel<kAll, 1, false, true, false>>(s, st, a);
-      return vec ? launch_rows<block_norm_kernel<kAll, 4, true, true, false>>(s, st, a) : launch_rows<block_norm_kernel<kAll, 4, false, true, false>>(s, st, a);
-    case kRowAsync:
-      return s.pieces == 4 ? launch_rows<block_norm_kernel<kAll, 4, true, false, true>>(s, st, a) : launch_rows<block_norm_kernel<kAll, 8, true, false, true>>(s, st, a);
-    default:
-      if (s.pieces == 1) return vec ? launch_rows<block_norm_kernel<kAll, 1, true, false, false>>(s, st, a) : launch_rows<block_norm_kernel<kAll, 1, false, false, false>>(s, st, a);
-      if (s.pieces == 2) return vec ? launch_rows<block_norm_kernel<kAll, 2, true, false, false>>(s, st, a) : launch_rows<block_norm_kernel<kAll, 2, false, false, false>>(s, st, a);
-      if (s.pieces == 4) return vec ? launch_rows<block_norm_kernel<kAll, 4, true, false, false>>(s, st, a) : launch_rows<block_norm_kernel<kAll, 4, false, false, false>>(s, st, a);
-      return launch_rows<block_norm_kernel<kAll, 8, false, false, false>>(s, st, a);
-  }
+  return vec ? launch_norm_as<kAll, true>(a, s, st) : launch_norm_as<kAll, false>(a, s, st);
 }
 
 }  // namespace stb
@@ -849,7 +845,7 @@ extern "C" int stb_quantize_i8(const void* x, size_t ldx, const void* x2, size_t
   const int bytes = stb::dtype_bytes(xdt);
   const bool vec = m % stb::kPiece == 0 && stb::rows_aligned(x, ldx, bytes, 16) && stb::rows_aligned(x2, ldx2, bytes, 16) && stb::rows_aligned(q, ldq, 1, 8);
   const stb::QuantI8Args a = {x, x2, rows, m, ldx, ldx2, ldq, q, scale};
-  const stb::RowShape s = stb::row_shape(m, rows, vec, xdt == STB_F32 || x2 ? 32u : 16u, 4u * 128u, 1024, x2 ? 0 : (xdt == STB_F32 ? 512 : 1024), x2 ? 1024 : 512);
+  const stb::RowShape s = stb::row_shape(m, rows, vec, {xdt == STB_F32 || x2 ? 32u : 16u, 4u * 128u, 1024, x2 ? 0 : (xdt == STB_F32 ? 512 : 1024), x2 ? 1024 : 512, 4});
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool half = xdt == STB_F16;
   const cudaError_t e = x2 ? (half ? stb::launch_quantize<STB_F16, true>(a, s, vec, st) : stb::launch_quantize<STB_BF16, true>(a, s, vec, st))
@@ -883,8 +879,8 @@ extern "C" int stb_block_norm(const stb_norm* args, void* stream) {
                    stb::rows_aligned(a.y, a.ldy, yb, 16) && stb::rows_aligned(a.q, a.ldq, 1, 8) && stb::rows_aligned(a.gate, a.tokens > a.tokens_per_gate ? a.ldgate : 0, wb, 16) &&
                    stb::rows_aligned(a.post_weight, 0, wb, 16) && stb::rows_aligned(a.post_bias, 0, wb, 16) && stb::rows_aligned(a.weight, 0, wb, 16) &&
                    stb::rows_aligned(a.bias, 0, wb, 16);
-  const uint32_t slot = (a.xdt == STB_F32 ? 32u : 16u) + (!a.resid ? 0u : (a.rdt == STB_F32 ? 32u : 16u));
-  const stb::RowShape s = stb::row_shape(a.h, a.tokens, vec, slot, 10u * 128u, 1024, 512);
+  const uint32_t each = (a.xdt == STB_F32 ? 32u : 16u) + (!a.resid ? 0u : (a.rdt == STB_F32 ? 32u : 16u));
+  const stb::RowShape s = stb::row_shape(a.h, a.tokens, vec, {each, 10u * 128u, 1024, 512, 512, 2});
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool same = a.xdt != STB_F32 && (!residual || a.rdt == a.xdt) && (!vectors || a.wdt == a.xdt);
   const cudaError_t e = !same ? stb::launch_norm<stb::kAnyType>(a, s, vec, st) : (a.xdt == STB_F16 ? stb::launch_norm<STB_F16>(a, s, vec, st) : stb::launch_norm<STB_BF16>(a, s, vec, st));
