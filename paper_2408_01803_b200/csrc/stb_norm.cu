@@ -101,8 +101,9 @@ __device__ __forceinline__ void values_of(const RawPiece<kType>& r, float (&v)[k
     unpack_piece<kType>(r.w[0], v);
   }
 }
-// Piece p of the row that starts at `row`: zeros behind its end.
-template <int kType, bool kVec>
+// Piece p of the row that starts at `row`: zeros behind its end.  kClamp: values without 16-byte pieces are read at a clamped place, without branches, so that the
+// loads of several rows stay together (norms: 1000 x 5111 26 -> 17 us; the quantizer has one row to read and is faster without the clamps, 13 -> 9).
+template <int kType, bool kVec, bool kClamp>
 __device__ __forceinline__ RawPiece<kType> load_piece(const RowPlace<kVec>& pl, const void* row, int p) {
   RawPiece<kType> r;
   constexpr int kParts = kType == STB_F32 ? 2 : 1;
@@ -115,17 +116,24 @@ __device__ __forceinline__ RawPiece<kType> load_piece(const RowPlace<kVec>& pl, 
 #pragma unroll
       for (int h = 0; h < kParts; ++h) r.w[h] = q[h];
     }
-  } else if constexpr (kType == STB_F32) {
-    uint32_t u[kPiece];
-#pragma unroll
-    for (int k = 0; k < kPiece; ++k) u[k] = pl.at(p, k) < pl.m ? static_cast<const uint32_t*>(row)[pl.at(p, k)] : 0u;
-    r.w[0] = make_uint4(u[0], u[1], u[2], u[3]);
-    r.w[1] = make_uint4(u[4], u[5], u[6], u[7]);
   } else {
     uint32_t u[kPiece];
 #pragma unroll
-    for (int k = 0; k < kPiece; ++k) u[k] = pl.at(p, k) < pl.m ? static_cast<const unsigned short*>(row)[pl.at(p, k)] : 0u;
-    r.w[0] = make_uint4(u[0] | (u[1] << 16), u[2] | (u[3] << 16), u[4] | (u[5] << 16), u[6] | (u[7] << 16));
+    for (int k = 0; k < kPiece; ++k) {
+      const int e = kClamp ? min(pl.at(p, k), pl.m - 1) : pl.at(p, k);
+      u[k] = 0u;
+      if (kClamp || e < pl.m) u[k] = kType == STB_F32 ? static_cast<const uint32_t*>(row)[e] : (uint32_t)static_cast<const unsigned short*>(row)[e];
+    }
+    if (kClamp) {
+#pragma unroll
+      for (int k = 0; k < kPiece; ++k) u[k] = pl.at(p, k) < pl.m ? u[k] : 0u;
+    }
+    if constexpr (kType == STB_F32) {
+      r.w[0] = make_uint4(u[0], u[1], u[2], u[3]);
+      r.w[1] = make_uint4(u[4], u[5], u[6], u[7]);
+    } else {
+      r.w[0] = make_uint4(u[0] | (u[1] << 16), u[2] | (u[3] << 16), u[4] | (u[5] << 16), u[6] | (u[7] << 16));
+    }
   }
   return r;
 }
@@ -139,7 +147,7 @@ __device__ __forceinline__ void for_row(const RowPlace<kVec>& pl, const void* ro
     for (int p0 = 0; p0 < P; p0 += kAtOnce) {
       RawPiece<kType> raw[kAtOnce];
 #pragma unroll
-      for (int p = 0; p < kAtOnce; ++p) raw[p] = load_piece<kType, kVec>(pl, row, p0 + p);
+      for (int p = 0; p < kAtOnce; ++p) raw[p] = load_piece<kType, kVec, true>(pl, row, p0 + p);
 #pragma unroll
       for (int p = 0; p < kAtOnce; ++p) {
         float u[kPiece];
@@ -149,15 +157,33 @@ __device__ __forceinline__ void for_row(const RowPlace<kVec>& pl, const void* ro
     }
   });
 }
+// A row as it lies in memory, asked for; and, later, f(p, values) for its pieces.
+template <int P> struct RawRow { uint4 w[P][2]; };
 template <int kAll, int P, bool kVec>
-__device__ __forceinline__ void load_row(const RowPlace<kVec>& pl, const void* row, int dt, float (&v)[P][kPiece]) {
+__device__ __forceinline__ void ask_raw(const RowPlace<kVec>& pl, const void* row, int dt, RawRow<P>& raw) {
   by_type<kAll>(dt, [&](auto type) {
     constexpr int kType = decltype(type)::value;
-    RawPiece<kType> raw[P];
 #pragma unroll
-    for (int p = 0; p < P; ++p) raw[p] = load_piece<kType, kVec>(pl, row, p);
+    for (int p = 0; p < P; ++p) {
+      const RawPiece<kType> r = load_piece<kType, kVec, true>(pl, row, p);
+      raw.w[p][0] = r.w[0];
+      if constexpr (kType == STB_F32) raw.w[p][1] = r.w[1];
+    }
+  });
+}
+template <int kAll, int P, class F>
+__device__ __forceinline__ void for_raw(const RawRow<P>& raw, int dt, F f) {
+  by_type<kAll>(dt, [&](auto type) {
+    constexpr int kType = decltype(type)::value;
 #pragma unroll
-    for (int p = 0; p < P; ++p) values_of<kType>(raw[p], v[p]);
+    for (int p = 0; p < P; ++p) {
+      RawPiece<kType> r;
+      r.w[0] = raw.w[p][0];
+      if constexpr (kType == STB_F32) r.w[1] = raw.w[p][1];
+      float u[kPiece];
+      values_of<kType>(r, u);
+      f(p, u);
+    }
   });
 }
 template <int kAll, int P, bool kVec>
@@ -506,8 +532,8 @@ quantize_i8_kernel(const QuantI8Args args) {
     if constexpr (!kAsync) {
 #pragma unroll
       for (int p = 0; p < P; ++p) {
-        raw[p] = load_piece<kType, kVec>(pl, row_x(row), p);
-        if constexpr (kGated) raw2[p] = load_piece<kType, kVec>(pl, row_x2(row), p);
+        raw[p] = load_piece<kType, kVec, false>(pl, row_x(row), p);
+        if constexpr (kGated) raw2[p] = load_piece<kType, kVec, false>(pl, row_x2(row), p);
       }
     }
     if constexpr (kType == STB_F32) {
@@ -593,10 +619,10 @@ quantize_i8_long_kernel(const QuantI8Args args) {
   float v[1][kPiece];
   auto read = [&](int base) {
     pl.m = args.m - base;
-    values_of<kType>(load_piece<kType, kVec>(pl, xr + (size_t)base * kBytes, 0), v[0]);
+    values_of<kType>(load_piece<kType, kVec, false>(pl, xr + (size_t)base * kBytes, 0), v[0]);
     if constexpr (kGated) {
       float b[kPiece];
-      values_of<kType>(load_piece<kType, kVec>(pl, xr2 + (size_t)base * kBytes, 0), b);
+      values_of<kType>(load_piece<kType, kVec, false>(pl, xr2 + (size_t)base * kBytes, 0), b);
 #pragma unroll
       for (int k = 0; k < kPiece; k += 2) {
         uint32_t lo, hi;
@@ -644,14 +670,6 @@ __device__ __forceinline__ void norm_row(const RowPlace<kVec>& pl, float (&v)[P]
 #pragma unroll
     for (int k = 0; k < kPiece; k += 2) mul_two(v[p][k], v[p][k + 1], v[p][k], v[p][k + 1], inv, inv);
 }
-// v = f(v, the row at w), two at a time
-template <int kAll, int P, bool kVec, class F>
-__device__ __forceinline__ void with_row(const RowPlace<kVec>& pl, float (&v)[P][kPiece], const void* w, int dt, F f) {
-  for_row<kAll, P, kVec>(pl, w, dt, [&](int p, const float (&u)[kPiece]) {
-#pragma unroll
-    for (int k = 0; k < kPiece; k += 2) f(v[p][k], v[p][k + 1], u[k], u[k + 1]);
-  });
-}
 // kAll: the type of x, the residual and the weights, where it is the same 16-bit type.
 template <int kAll, int P, bool kVec, bool kWarp, bool kAsync>
 __global__ void __launch_bounds__(kWarp ? 256 : (kAsync || (!kVec && P > 2) ? 512 : kMaxRowThreads), kWarp || (kAsync && P <= 4) ? 2 : 1)
@@ -673,46 +691,69 @@ block_norm_kernel(const __grid_constant__ stb_norm a) {
   };
   if (kAsync && row < a.tokens) ask(row);
   for (; row < a.tokens; row += stride, slot ^= 5) {
-    constexpr bool kEarly = !kAsync && (kWarp || P <= 2);       // the residual's loads beside those of x, where registers hold both
-    float v[P][kPiece], r[kEarly ? P : 1][kPiece];
+    // What is asked for before the first sum: the residual beside x, and the vectors, as far as registers hold them.
+    constexpr bool kEarly = !kAsync && (kWarp || P <= 2), kAhead = kVec && !kAsync && (P == 1 || (P == 2 && kAll != kAnyType));
+    float v[P][kPiece];
+    RawRow<kEarly ? P : 1> raw_r;
+    RawRow<kAhead ? P : 1> raw_pw, raw_gate, raw_w;
+    const char* gate_row = row_of(gate, gate ? row / a.tokens_per_gate : 0, a.ldgate, a.wdt);
+    auto take = [&](int p, const float (&u)[kPiece]) {
+#pragma unroll
+      for (int k = 0; k < kPiece; ++k) v[p][k] = u[k];
+    };
+    auto times = [&](int p, const float (&u)[kPiece]) {
+#pragma unroll
+      for (int k = 0; k < kPiece; k += 2) mul_two(v[p][k], v[p][k + 1], v[p][k], v[p][k + 1], u[k], u[k + 1]);
+    };
+    auto plus = [&](int p, const float (&u)[kPiece]) {
+#pragma unroll
+      for (int k = 0; k < kPiece; k += 2) add_two(v[p][k], v[p][k + 1], v[p][k], v[p][k + 1], u[k], u[k + 1]);
+    };
+    auto onto = [&](int p, const float (&u)[kPiece]) {
+#pragma unroll
+      for (int k = 0; k < kPiece; k += 2) fma_two(v[p][k], v[p][k + 1], v[p][k], v[p][k + 1], a.alpha, a.alpha, u[k], u[k + 1]);
+    };
     if constexpr (kAsync) {
       copy_async_done();
-      for_slots<kAll, P>(pl, a.xdt, slot_x, [&](int p, const float (&u)[kPiece]) {
-#pragma unroll
-        for (int k = 0; k < kPiece; ++k) v[p][k] = u[k];
-      });
-    } else {
-      load_row<kAll, P, kVec>(pl, row_of(x, row, a.ldx, a.xdt), a.xdt, v);
-      if constexpr (kEarly) {
-        if (resid) load_row<kAll, P, kVec>(pl, row_of(resid, row, a.ldr, a.rdt), a.rdt, r);
+      for_slots<kAll, P>(pl, a.xdt, slot_x, take);
+    } else if constexpr (kEarly) {
+      RawRow<P> raw_x;
+      ask_raw<kAll, P, kVec>(pl, row_of(x, row, a.ldx, a.xdt), a.xdt, raw_x);
+      if (resid) ask_raw<kAll, P, kVec>(pl, row_of(resid, row, a.ldr, a.rdt), a.rdt, raw_r);
+      if constexpr (kAhead) {
+        if (pw) ask_raw<kAll, P, kVec>(pl, pw, a.wdt, raw_pw);
+        if (gate) ask_raw<kAll, P, kVec>(pl, gate_row, a.wdt, raw_gate);
+        if (w) ask_raw<kAll, P, kVec>(pl, w, a.wdt, raw_w);
       }
+      for_raw<kAll, P>(raw_x, a.xdt, take);
+    } else {
+      for_row<kAll, P, kVec>(pl, row_of(x, row, a.ldx, a.xdt), a.xdt, take);
     }
-    auto times = [](float& v0, float& v1, float f0, float f1) { mul_two(v0, v1, v0, v1, f0, f1); };
-    auto plus = [](float& v0, float& v1, float f0, float f1) { add_two(v0, v1, v0, v1, f0, f1); };
-    auto onto = [&](float& v0, float& v1, float r0, float r1) { fma_two(v0, v1, v0, v1, a.alpha, a.alpha, r0, r1); };
     if (a.post) {
       norm_row<P, kVec, kWarp>(pl, v, a.kind, a.eps, sh, slot);
-      if (pw) with_row<kAll, P, kVec>(pl, v, pw, a.wdt, times);
-      if (pb) with_row<kAll, P, kVec>(pl, v, pb, a.wdt, plus);
+      if constexpr (kAhead) {
+        if (pw) for_raw<kAll, P>(raw_pw, a.wdt, times);
+      } else {
+        if (pw) for_row<kAll, P, kVec>(pl, pw, a.wdt, times);
+      }
+      if (pb) for_row<kAll, P, kVec>(pl, pb, a.wdt, plus);
     }
-    if (gate) with_row<kAll, P, kVec>(pl, v, row_of(gate, row / a.tokens_per_gate, a.ldgate, a.wdt), a.wdt, times);
+    if constexpr (kAhead) {
+      if (gate) for_raw<kAll, P>(raw_gate, a.wdt, times);
+    } else {
+      if (gate) for_row<kAll, P, kVec>(pl, gate_row, a.wdt, times);
+    }
     if (!resid) {
 #pragma unroll
       for (int p = 0; p < P; ++p)
 #pragma unroll
         for (int k = 0; k < kPiece; ++k) v[p][k] *= a.alpha;
     } else if constexpr (kEarly) {
-#pragma unroll
-      for (int p = 0; p < P; ++p)
-#pragma unroll
-        for (int k = 0; k < kPiece; k += 2) onto(v[p][k], v[p][k + 1], r[p][k], r[p][k + 1]);
+      for_raw<kAll, P>(raw_r, a.rdt, onto);
     } else if constexpr (kAsync) {
-      for_slots<kAll, P>(pl, a.rdt, slot_r, [&](int p, const float (&u)[kPiece]) {
-#pragma unroll
-        for (int k = 0; k < kPiece; k += 2) onto(v[p][k], v[p][k + 1], u[k], u[k + 1]);
-      });
+      for_slots<kAll, P>(pl, a.rdt, slot_r, onto);
     } else {
-      with_row<kAll, P, kVec>(pl, v, row_of(resid, row, a.ldr, a.rdt), a.rdt, onto);
+      for_row<kAll, P, kVec>(pl, row_of(resid, row, a.ldr, a.rdt), a.rdt, onto);
     }
     if (a.resid_out) store_row<kAll, P, kVec>(pl, const_cast<char*>(row_of(a.resid_out, row, a.ldro, a.rdt)), a.rdt, v);
     const bool more = kAsync && row + stride < a.tokens;
@@ -722,8 +763,12 @@ block_norm_kernel(const __grid_constant__ stb_norm a) {
     }
     norm_row<P, kVec, kWarp>(pl, v, a.kind, a.eps, sh, slot + 2);
     if (more) ask(row + stride);                   // (this row's pieces have been read: its sum is known)
-    if (w) with_row<kAll, P, kVec>(pl, v, w, a.wdt, times);
-    if (b) with_row<kAll, P, kVec>(pl, v, b, a.wdt, plus);
+    if constexpr (kAhead) {
+      if (w) for_raw<kAll, P>(raw_w, a.wdt, times);
+    } else {
+      if (w) for_row<kAll, P, kVec>(pl, w, a.wdt, times);
+    }
+    if (b) for_row<kAll, P, kVec>(pl, b, a.wdt, plus);
     if (a.y) store_row<kAnyType, P, kVec>(pl, const_cast<char*>(row_of(a.y, row, a.ldy, a.ydt)), a.ydt, v);
     if (a.q) {
       const RowScale s = row_scale(row_max<kWarp>(max_bits<P>(v), sh, slot + 4));
@@ -735,7 +780,7 @@ block_norm_kernel(const __grid_constant__ stb_norm a) {
 
 // ---- launches -----------------------------------------------------------------------------------------------------------------------
 // How rows of m values are dealt out.
-//   warp:    rows of up to 256 values, or of up to 1024 where there are more than SMs; 1 or 4 pieces per lane
+//   warp:    rows of up to 256 values, or of up to 1024 where there are more than SMs; 1, 2 or 4 pieces per lane
 //   slots:   the next row on its way into shared memory: more than 296 rows that can be read in 16-byte pieces, 4 or 8 pieces per thread, whichever fills
 //            an SM better (resident4, resident8: the threads that its registers take; most4: a CTA's with 4), as many CTAs as stay on the GPU
 //   else:    one CTA per row, with one piece per thread as long as 1024 threads reach, for the shortest way through a row; `any_pieces` of them where there are
@@ -749,7 +794,7 @@ static RowShape row_shape(int m, int rows, bool vec, const RowNeeds& need) {
   if (m <= 256 || (m <= 1024 && rows > 148)) {
     const int per_cta = rows >= 148 * 8 ? 8 : (rows >= 148 * 2 ? 2 : 1);
     s.warp = true;
-    s.pieces = pieces <= 32 ? 1 : 4;
+    s.pieces = pieces <= 32 ? 1 : (pieces <= 64 ? 2 : 4);
     s.threads = 32 * per_cta;
     s.grid = (rows + per_cta - 1) / per_cta;
     return s;
@@ -801,7 +846,10 @@ static cudaError_t launch_rows(const RowShape& s, cudaStream_t st, const A& args
 template <int kType, bool kGated, bool kVec>
 static cudaError_t launch_quantize_as(const QuantI8Args& a, const RowShape& s, cudaStream_t st) {
   if (s.longer) return launch_rows<quantize_i8_long_kernel<kType, kGated, kVec>>(s, st, a);
-  if (s.warp) return s.pieces == 1 ? launch_rows<quantize_i8_kernel<1, kType, kGated, kVec, true, false>>(s, st, a) : launch_rows<quantize_i8_kernel<4, kType, kGated, kVec, true, false>>(s, st, a);
+  if (s.warp) {
+    if (s.pieces == 1) return launch_rows<quantize_i8_kernel<1, kType, kGated, kVec, true, false>>(s, st, a);
+    return s.pieces == 2 ? launch_rows<quantize_i8_kernel<2, kType, kGated, kVec, true, false>>(s, st, a) : launch_rows<quantize_i8_kernel<4, kType, kGated, kVec, true, false>>(s, st, a);
+  }
   if constexpr (kVec) {
     if constexpr (!kGated) {
       if (s.slots && s.pieces == 8) return launch_rows<quantize_i8_kernel<8, kType, kGated, true, false, true>>(s, st, a);
@@ -820,7 +868,10 @@ static cudaError_t launch_quantize(const QuantI8Args& a, const RowShape& s, bool
 }
 template <int kAll, bool kVec>
 static cudaError_t launch_norm_as(const stb_norm& a, const RowShape& s, cudaStream_t st) {
-  if (s.warp) return s.pieces == 1 ? launch_rows<block_norm_kernel<kAll, 1, kVec, true, false>>(s, st, a) : launch_rows<block_norm_kernel<kAll, 4, kVec, true, false>>(s, st, a);
+  if (s.warp) {
+    if (s.pieces == 1) return launch_rows<block_norm_kernel<kAll, 1, kVec, true, false>>(s, st, a);
+    return s.pieces == 2 ? launch_rows<block_norm_kernel<kAll, 2, kVec, true, false>>(s, st, a) : launch_rows<block_norm_kernel<kAll, 4, kVec, true, false>>(s, st, a);
+  }
   if constexpr (kVec) {
     if (s.slots) return s.pieces == 4 ? launch_rows<block_norm_kernel<kAll, 4, true, false, true>>(s, st, a) : launch_rows<block_norm_kernel<kAll, 8, true, false, true>>(s, st, a);
   }
@@ -879,10 +930,10 @@ extern "C" int stb_block_norm(const stb_norm* args, void* stream) {
                    stb::rows_aligned(a.y, a.ldy, yb, 16) && stb::rows_aligned(a.q, a.ldq, 1, 8) && stb::rows_aligned(a.gate, a.tokens > a.tokens_per_gate ? a.ldgate : 0, wb, 16) &&
                    stb::rows_aligned(a.post_weight, 0, wb, 16) && stb::rows_aligned(a.post_bias, 0, wb, 16) && stb::rows_aligned(a.weight, 0, wb, 16) &&
                    stb::rows_aligned(a.bias, 0, wb, 16);
+  const bool same = a.xdt != STB_F32 && (!residual || a.rdt == a.xdt) && (!vectors || a.wdt == a.xdt);
   const uint32_t each = (a.xdt == STB_F32 ? 32u : 16u) + (!a.resid ? 0u : (a.rdt == STB_F32 ? 32u : 16u));
   const stb::RowShape s = stb::row_shape(a.h, a.tokens, vec, {each, 10u * 128u, 1024, 512, 512, 2});
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const bool same = a.xdt != STB_F32 && (!residual || a.rdt == a.xdt) && (!vectors || a.wdt == a.xdt);
   const cudaError_t e = !same ? stb::launch_norm<stb::kAnyType>(a, s, vec, st) : (a.xdt == STB_F16 ? stb::launch_norm<STB_F16>(a, s, vec, st) : stb::launch_norm<STB_BF16>(a, s, vec, st));
   return e == cudaSuccess ? STB_OK : STB_ERR_CUDA;
 }
