@@ -381,18 +381,20 @@ __device__ __forceinline__ void store_row_i8(const RowPlace<kVec>& pl, int8_t* r
   }
 }
 
-// ---- the gated activation ---------------------------------------------------------------------------------------------------------
-// silu(a) b rounded to fp32 and then to the 16-bit type, as exact arithmetic would.  In fp32 it is known within (5 + 0.75 |min(a, 0)|) 2^-23 (in units of 2^-23: the power
-// of two 2 by its specification and 0.75 |a| from its rounded argument, of which e / (1 + e) reaches the result, the reciprocal 1, the sum, the two products and the
-// fp32 rounding half a one each; a >= -80, where nothing leaves fp32's range): both ends of a band somewhat wider are rounded, and nearly always give the same 16-bit value.  Where they
-// do not, that of the smaller magnitude is kept, the other is the next one up, and the pair is marked: it is evaluated in float64 only where the
-// choice would show, in the row's largest magnitude or in the value's 8 bits.
 // the larger of each half
 __device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
+
+// ---- the gated activation ---------------------------------------------------------------------------------------------------------
+// silu(a) b rounded to fp32 and then to the 16-bit type, as exact arithmetic would.  In fp32 it is known within (5 + 0.75 |min(a, 0)|) 2^-23 (in units of
+// 2^-23: the power of two 2 by its specification and 0.75 |a| from its rounded argument, of which e / (1 + e) reaches the result, the reciprocal 1,
+// the sum, the two products and the fp32 rounding half a one each; a >= -80, where nothing leaves fp32's range): both ends of a band somewhat wider are
+// rounded, and nearly always give the same 16-bit value.  Where they do not, that of the smaller magnitude is kept, the other is the next one up, and the
+// pair is marked: it is evaluated in float64 only where the choice would show, in the row's largest magnitude or in the value's 8 bits.  (Everything in
+// float64 would be 150 instructions a value; this way the whole kernel has 35.)
 template <int kType>
 __device__ __noinline__ uint32_t gated_exact(float a0, float a1, float b0, float b1) {
   const double d0 = (double)a0, d1 = (double)a1;
@@ -503,13 +505,15 @@ quantize_i8_kernel(const QuantI8Args args) {
   const void *x = args.x, *x2 = args.x2;
   begin_after(x, x2);
   constexpr int kBytes = kType == STB_F32 ? 4 : 2;
-  const int stride = kWarp ? (int)(gridDim.x * (blockDim.x >> 5)) : (int)gridDim.x;
-  int row = kWarp ? (int)(blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5)) : (int)blockIdx.x, slot = 0;
+  // (unsigned: a row behind the last one is below 2^32, whatever their number)
+  const uint32_t rows = (uint32_t)args.rows, stride = kWarp ? gridDim.x * (blockDim.x >> 5) : gridDim.x;
+  uint32_t row = kWarp ? blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : blockIdx.x;
+  int slot = 0;
   const RowPlace<kVec> pl{kWarp ? (int)(threadIdx.x & 31) : (int)threadIdx.x, kWarp ? 32 : (int)blockDim.x, args.m};
   uint8_t *slot_x = slots, *slot_x2 = slots + (size_t)(P * pl.width) * 16u;
-  auto row_x = [&](int r) { return static_cast<const char*>(x) + (size_t)r * args.ldx * kBytes; };
-  auto row_x2 = [&](int r) { return static_cast<const char*>(x2) + (size_t)r * args.ldx2 * kBytes; };
-  auto ask = [&](int r) {
+  auto row_x = [&](uint32_t r) { return static_cast<const char*>(x) + (size_t)r * args.ldx * kBytes; };
+  auto row_x2 = [&](uint32_t r) { return static_cast<const char*>(x2) + (size_t)r * args.ldx2 * kBytes; };
+  auto ask = [&](uint32_t r) {
     if constexpr (kAsync) {
       ask_row<kType, P>(pl, row_x(r), kType, slot_x);
       if (kGated) ask_row<kType, P>(pl, row_x2(r), kType, slot_x2);
@@ -522,8 +526,8 @@ quantize_i8_kernel(const QuantI8Args args) {
       r.h[p][0] = h.x; r.h[p][1] = h.y; r.h[p][2] = h.z; r.h[p][3] = h.w;
     }
   };
-  if (kAsync && row < args.rows) ask(row);
-  for (; row < args.rows; row += stride, slot ^= 2) {
+  if (kAsync && row < rows) ask(row);
+  for (; row < rows; row += stride, slot ^= 2) {
     QuantRow<P, kType> r;
     r.marks = 0;
     uint32_t bits;
@@ -574,7 +578,7 @@ quantize_i8_kernel(const QuantI8Args args) {
       }
       bits = magnitude_bits<kType>(largest);
     }
-    if (kAsync && row + stride < args.rows) ask(row + stride);        // (this row's pieces have been read: its largest magnitude is known)
+    if (kAsync && row + stride < rows) ask(row + stride);        // (this row's pieces have been read: its largest magnitude is known)
     const RowScale s = row_scale(bits);
     int8_t* qr = args.q + (size_t)row * args.ldq;
     if (pl.lane == 0) args.scale[row] = s.scale;
@@ -678,25 +682,27 @@ block_norm_kernel(const __grid_constant__ stb_norm a) {
   __shared__ float sh[10][32];                      // the parts of a row's five reductions, and of the next one's
   const void *x = a.x, *resid = a.resid, *pw = a.post_weight, *pb = a.post_bias, *gate = a.gate, *w = a.weight, *b = a.bias;
   begin_after(x, resid, pw, pb, gate, w, b);
-  const int stride = kWarp ? (int)(gridDim.x * (blockDim.x >> 5)) : (int)gridDim.x;
-  int row = kWarp ? (int)(blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5)) : (int)blockIdx.x, slot = 0;
+  // (unsigned: a row behind the last one is below 2^32, whatever their number)
+  const uint32_t rows = (uint32_t)a.tokens, stride = kWarp ? gridDim.x * (blockDim.x >> 5) : gridDim.x;
+  uint32_t row = kWarp ? blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : blockIdx.x;
+  int slot = 0;
   const RowPlace<kVec> pl{kWarp ? (int)(threadIdx.x & 31) : (int)threadIdx.x, kWarp ? 32 : (int)blockDim.x, a.h};
   auto row_of = [&](const void* base, size_t r, size_t ld, int dt) { return static_cast<const char*>(base) + r * ld * (size_t)dtype_bytes(dt); };
   uint8_t *slot_x = slots, *slot_r = slots + (size_t)(P * pl.width) * ((kAll == kAnyType ? a.xdt : kAll) == STB_F32 ? 32u : 16u);
-  auto ask = [&](int r) {
+  auto ask = [&](uint32_t r) {
     if constexpr (kAsync) {
       ask_row<kAll, P>(pl, row_of(x, r, a.ldx, a.xdt), a.xdt, slot_x);
       if (resid) ask_row<kAll, P>(pl, row_of(resid, r, a.ldr, a.rdt), a.rdt, slot_r);
     }
   };
-  if (kAsync && row < a.tokens) ask(row);
-  for (; row < a.tokens; row += stride, slot ^= 5) {
+  if (kAsync && row < rows) ask(row);
+  for (; row < rows; row += stride, slot ^= 5) {
     // What is asked for before the first sum: the residual beside x, and the vectors, as far as registers hold them.
     constexpr bool kEarly = !kAsync && (kWarp || P <= 2), kAhead = kVec && !kAsync && (P == 1 || (P == 2 && kAll != kAnyType));
     float v[P][kPiece];
     RawRow<kEarly ? P : 1> raw_r;
     RawRow<kAhead ? P : 1> raw_pw, raw_gate, raw_w;
-    const char* gate_row = row_of(gate, gate ? row / a.tokens_per_gate : 0, a.ldgate, a.wdt);
+    const char* gate_row = row_of(gate, gate ? row / (uint32_t)a.tokens_per_gate : 0u, a.ldgate, a.wdt);
     auto take = [&](int p, const float (&u)[kPiece]) {
 #pragma unroll
       for (int k = 0; k < kPiece; ++k) v[p][k] = u[k];
@@ -756,7 +762,7 @@ block_norm_kernel(const __grid_constant__ stb_norm a) {
       for_row<kAll, P, kVec>(pl, row_of(resid, row, a.ldr, a.rdt), a.rdt, onto);
     }
     if (a.resid_out) store_row<kAll, P, kVec>(pl, const_cast<char*>(row_of(a.resid_out, row, a.ldro, a.rdt)), a.rdt, v);
-    const bool more = kAsync && row + stride < a.tokens;
+    const bool more = kAsync && row + stride < rows;
     if (!a.y && !a.q) {
       if (more) ask(row + stride);
       continue;
@@ -796,7 +802,7 @@ static RowShape row_shape(int m, int rows, bool vec, const RowNeeds& need) {
     s.warp = true;
     s.pieces = pieces <= 32 ? 1 : (pieces <= 64 ? 2 : 4);
     s.threads = 32 * per_cta;
-    s.grid = (rows + per_cta - 1) / per_cta;
+    s.grid = (int)(((long long)rows + per_cta - 1) / per_cta);
     return s;
   }
   if (vec && rows > 296) {
