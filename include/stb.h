@@ -295,7 +295,7 @@ int stb_quantize_i8(const void *x, size_t ldx, const void *x2, size_t ldx2, stb_
 
 /* The linear layer in 8 bits:  Y[t][i] = x_scale[t] w_scale[i] sum_j W[i][j] X[t][j] (+ bias[i]).  The sum is exact (int32; m <= 131071, else
  * STB_ERR_SHAPE), rounded to fp32, multiplied by x_scale[t], then by w_scale[i], then the bias is added, each in fp32, and the result is rounded
- * once to Y's type: every form of the kernel gives the same bits.  W: int8 [n][ldw], X: int8 [T][ldx]; n, m, T of any size from 1; ldw, ldx >= m
+ * once to Y's type: every form of the kernel gives the same bits.  W: int8 [n][ldw], X: int8 [T][ldx]; n, T of 1 to 2^30; ldw, ldx >= m
  * and multiples of 16, W and X 16-byte aligned (what lies behind the m-th value of a row is not read into the result); w_scale: fp32 [n],
  * x_scale: fp32 [T], bias: fp32 [n] or NULL; Y: fp32, fp16 or bf16 [T][ldy], ldy >= n.  No workspace.  dev_status: as for stb_gemm. */
 int stb_gemm_i8(const int8_t *W, size_t ldw, const float *w_scale, const float *bias, int n, int m, const int8_t *X, size_t ldx,

@@ -505,6 +505,8 @@ def _rows(t, like, where):
     _refuse(not t.is_cuda or t.device != like.device, "%s is on %s" % (where, t.device))
     t2 = t if t.dim() == 2 else t.unsqueeze(0)
     _refuse(t2.dim() != 2 or (t2.stride(1) != 1 and t2.shape[1] > 1), "%s: rows of values side by side are needed" % where)
+    if max(t2.shape) > 0x7FFFFFFF:                  # (the library's sizes are of 32 bits)
+        raise StbError(STB_ERR_SHAPE, "%s: %d x %d" % (where, t2.shape[0], t2.shape[1]))
     return t2
 
 

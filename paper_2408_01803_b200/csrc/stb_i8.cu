@@ -16,6 +16,8 @@ namespace cg = cooperative_groups;
 
 namespace stb {
 
+constexpr int kI8MaxSide = 1 << 30;      // of n and T: tiles and what lies behind the last one are counted in 32 bits
+
 struct I8Args {
   const int8_t *W, *X;
   const float *w_scale, *bias, *x_scale;
@@ -391,9 +393,8 @@ static I8Plan i8_plan(int n, int m, int T) {
   }
   if (T > 48) {
     const float bytes = (weights + tokens + out) * (0.82f / 6.3e6f);
-    for (int tt = least; tt <= (T + 63) / 64; ++tt) {
-      const int bn = ((T + tt - 1) / tt + 31) / 32 * 32;
-      if (bn > 256 || bn < 64 || (tt - 1) * bn >= T) continue;
+    for (int bn = 256; bn >= 64; bn -= 32) {        // (seven choices however many tokens there are)
+      const int tt = (T + bn - 1) / bn;
       const float turns = (float)(((long long)((mtiles + 1) / 2) * tt + 73) / 74), sm = turns * (float)stages * (0.1336f + 0.000532f * (float)bn);
       const float cost = 2.0f + sqrtf(sm * sm + bytes * bytes) + 0.0567f * (float)bn + (turns - 1.0f) * (3.07f + 0.0047f * (float)bn);
       if (cost < best_cost) { best_cost = cost; best = {true, false, bn, tt, 0}; }
@@ -709,7 +710,7 @@ static int launch_i8_prefill(const I8Args& a, const I8Plan& plan, int* dev_statu
 extern "C" int stb_gemm_i8(const int8_t* W, size_t ldw, const float* w_scale, const float* bias, int n, int m, const int8_t* X, size_t ldx,
                            const float* x_scale, int T, void* Y, stb_dtype ydt, size_t ldy, int* dev_status, void* stream) {
   if (!W || !w_scale || !X || !x_scale || !Y) return STB_ERR_ARG;
-  if (n < 1 || m < 1 || T < 1 || m > 131071) return STB_ERR_SHAPE;
+  if (n < 1 || m < 1 || T < 1 || m > 131071 || n > stb::kI8MaxSide || T > stb::kI8MaxSide) return STB_ERR_SHAPE;
   if (ydt != STB_F32 && ydt != STB_F16 && ydt != STB_BF16) return STB_ERR_UNSUPPORTED;
   if (ldw < (size_t)m || ldx < (size_t)m || ldy < (size_t)n || (ldw % 16) != 0 || (ldx % 16) != 0) return STB_ERR_ARG;
   const uintptr_t small = ydt == STB_F32 ? 3u : 1u;

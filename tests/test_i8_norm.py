@@ -117,6 +117,34 @@ def test_python_calls_refuse_what_is_not_on_one_device(stb):
         assert e.value.status == stb.STB_ERR_ARG
 
 
+def test_gemm_i8_refuses_sides_beyond_its_range(stb):
+    """n and T of more than 2^30: what lies behind the last tile would pass 32 bits."""
+    one, top = C.c_void_p(256), (1 << 31) - 1
+    for n, T in ((top, 1), ((1 << 30) + 1, 8), (64, (1 << 30) + 1), (1, top)):
+        assert stb._lib.stb_gemm_i8(one, 64, one, None, n, 64, one, 64, one, T, one, stb.STB_F32, n, None, None) == stb.STB_ERR_SHAPE, (n, T)
+
+
+def test_python_calls_refuse_sides_beyond_32_bits(stb):
+    """Sizes that the library's int cannot hold are refused, not cut to their low 32 bits."""
+    class Matrix:
+        is_cuda, device, dtype = True, torch.device("cuda", 0), torch.int8
+
+        def __init__(self, *shape):
+            self.shape = shape
+
+        def dim(self):
+            return 2
+
+        def stride(self, i):
+            return (self.shape[1], 1)[i]
+
+    for shape in (((1 << 32) + 5, 1), (3, (1 << 32) + 16), (1 << 31, 1)):
+        with pytest.raises(stb.StbError) as e:
+            stb._rows(Matrix(*shape), Matrix(1, 1), "x")
+        assert e.value.status == stb.STB_ERR_SHAPE
+    assert stb._rows(Matrix((1 << 31) - 1, 1), Matrix(1, 1), "x").shape[1] == 1
+
+
 # ---- rows in 8 bits -------------------------------------------------------------------------------------------------------------------
 WIDTHS = (1, 2, 7, 8, 9, 64, 255, 256, 257, 511, 1024, 1025, 2813, 4096, 8200, 16384, 16391, 32768, 32769, 40001)
 
