@@ -381,29 +381,34 @@ __device__ __forceinline__ void store_row_i8(const RowPlace<kVec>& pl, int8_t* r
   }
 }
 
-// the larger of each half
-__device__ __forceinline__ uint32_t max_halves(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
+// the larger magnitude of each half (a holds magnitudes; a NaN stays one)
+template <int kType>
+__device__ __forceinline__ uint32_t max_magnitudes(uint32_t a, uint32_t b) {
+  if (kType == STB_F16) {
+    const __half2 r = __hmax2_nan(*reinterpret_cast<const __half2*>(&a), __habs2(*reinterpret_cast<const __half2*>(&b)));
+    return *reinterpret_cast<const uint32_t*>(&r);
+  }
+  const __nv_bfloat162 r = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&a), __habs2(*reinterpret_cast<const __nv_bfloat162*>(&b)));
+  return *reinterpret_cast<const uint32_t*>(&r);
 }
 
 // ---- the gated activation ---------------------------------------------------------------------------------------------------------
 // silu(a) b rounded to fp32 and then to the 16-bit type, as exact arithmetic would.  In fp32 it is known within (5 + 0.75 |min(a, 0)|) 2^-23 (in units of
 // 2^-23: the power of two 2 by its specification and 0.75 |a| from its rounded argument, of which e / (1 + e) reaches the result, the reciprocal 1,
-// the sum, the two products and the fp32 rounding half a one each; a >= -80, where nothing leaves fp32's range): both ends of a band somewhat wider are
-// rounded, and nearly always give the same 16-bit value.  Where they do not, that of the smaller magnitude is kept, the other is the next one up, and the
-// pair is marked: it is evaluated in float64 only where the choice would show, in the row's largest magnitude or in the value's 8 bits.  (Everything in
-// float64 would be 150 instructions a value; this way the whole kernel has 35.)
+// the sum, the two products and the fp32 rounding half a one each; a >= -80, where nothing leaves fp32's range): both ends of a band somewhat wider, of
+// one width for the eight values of a piece, are rounded, and nearly always give the same 16-bit value.  Where they do not, that of the smaller magnitude is
+// kept, the other is the next one up, and the value is marked: it is evaluated in float64 only where the choice would show, in the row's largest magnitude
+// or in the value's 8 bits.  (Everything in float64 would be 150 instructions a value.)
 template <int kType>
 __device__ __noinline__ uint32_t gated_exact(float a0, float a1, float b0, float b1) {
   const double d0 = (double)a0, d1 = (double)a1;
   return pack_two<kType>((float)(d0 / (1.0 + exp(-d0)) * (double)b0), (float)(d1 / (1.0 + exp(-d1)) * (double)b1));
 }
 constexpr float kUlp = 1.1920929e-7f;               // 2^-23
+__device__ __forceinline__ float gated_band(float least) { return fmaf(fminf(least, 0.0f), -kUlp, 6.0f * kUlp); }
 template <int kType>
-__device__ __forceinline__ void gated_two(float a0, float a1, float b0, float b1, uint32_t& lo, uint32_t& hi) {
-  float t0, t1, h0, h1, band0, band1, l0, l1, m0, m1;
+__device__ __forceinline__ void gated_two(float a0, float a1, float b0, float b1, float band, uint32_t& lo, uint32_t& hi) {
+  float t0, t1, h0, h1, l0, l1, m0, m1;
   mul_two(t0, t1, a0, a1, -1.4426950408889634f, -1.4426950408889634f);
   asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(t0));
   asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(t1));
@@ -412,9 +417,8 @@ __device__ __forceinline__ void gated_two(float a0, float a1, float b0, float b1
   asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(t1));
   mul_two(h0, h1, a0, a1, t0, t1);
   mul_two(h0, h1, h0, h1, b0, b1);
-  fma_two(band0, band1, fminf(a0, 0.0f), fminf(a1, 0.0f), -kUlp, -kUlp, 6.0f * kUlp, 6.0f * kUlp);
-  fma_two(m0, m1, h0, h1, band0, band1, h0, h1);
-  fma_two(l0, l1, h0, h1, -band0, -band1, h0, h1);
+  fma_two(m0, m1, h0, h1, band, band, h0, h1);
+  fma_two(l0, l1, h0, h1, -band, -band, h0, h1);
   lo = pack_two<kType>(l0, l1);
   hi = pack_two<kType>(m0, m1);
 }
@@ -427,24 +431,28 @@ struct QuantI8Args {
   int8_t* q;
   float* scale;
 };
-// The values: of kType as they are, or (16-bit types) gated.  What a thread holds of a row between its largest magnitude and its 8 bits.  Gated pairs: h is
-// the candidate of smaller magnitude, bit 4 p + k of marks says that pair k of piece p has two.
-template <int P, int kType> struct QuantRow { uint32_t h[P][kPiece / 2]; uint32_t marks; };
-template <int P> struct QuantRow<P, STB_F32> { float v[P][kPiece]; uint32_t marks; };
+// The values: of kType as they are, or (16-bit types) gated.  What a thread holds of a row between its largest magnitude and its 8 bits.  Gated values: h is
+// the candidate of smaller magnitude, marks says which have two: bits 4 (p % 4) + k and 16 beyond it of word p / 4 the two values of pair k of piece p.
+template <int P, int kType> struct QuantRow {
+  uint32_t h[P][kPiece / 2], marks[(P + 3) / 4];
+  __device__ __forceinline__ uint32_t marks_of(int p) const { return (marks[p / 4] >> (4 * (p & 3))) & 0x000F000Fu; }
+};
+template <int P> struct QuantRow<P, STB_F32> { float v[P][kPiece]; };
 
-// Settles the marked pairs of a piece: in float64, from the inputs again, where the 8 bits depend on which of the two candidates it is (a magnitude's next
+// Settles the marked values of a piece: in float64, from the inputs again, where the 8 bits depend on which of the two candidates it is (a magnitude's next
 // one up: its bits plus one), or, inverse < 0, all of them.  The values lie at `at`, each `step` behind the one before it.
 template <int kType>
 __device__ __noinline__ uint4 settle_piece(uint4 h, uint32_t marks, const void* xr, const void* xr2, int at, int step, int m, float inverse, float largest) {
 #pragma unroll
   for (int k = 0; k < kPiece / 2; ++k) {
     uint32_t& two = k == 0 ? h.x : (k == 1 ? h.y : (k == 2 ? h.z : h.w));
-    if (!((marks >> k) & 1u)) continue;
+    const uint32_t here = (marks >> k) & 0x00010001u;
+    if (here == 0u) continue;
     bool shows = inverse < 0.0f;
     if (!shows) {
       float a, b, c, d;
       unpack_two<kType>(two, a, b);
-      unpack_two<kType>(two + 0x00010001u, c, d);
+      unpack_two<kType>(two + here, c, d);
       shows = value_i8_exact(a, inverse, largest) != value_i8_exact(c, inverse, largest) || value_i8_exact(b, inverse, largest) != value_i8_exact(d, inverse, largest);
     }
     const int i = at + 2 * k * step, j = i + step;
@@ -463,9 +471,14 @@ __device__ __noinline__ uint4 gated_exact_piece(uint4 ra, uint4 rb) {
   unpack_piece<kType>(rb, b);
   return make_uint4(gated_exact<kType>(a[0], a[1], b[0], b[1]), gated_exact<kType>(a[2], a[3], b[2], b[3]), gated_exact<kType>(a[4], a[5], b[4], b[5]), gated_exact<kType>(a[6], a[7], b[6], b[7]));
 }
-// The gated values of a piece.  top: per half the largest of 2 magnitude + (whether there are two candidates), of the larger candidates.
+__device__ __forceinline__ uint32_t one_where_any(uint32_t halves) {      // 1 in every half that is not zero
+  uint32_t r;
+  asm("min.u16x2 %0, %1, %2;" : "=r"(r) : "r"(halves), "r"(0x00010001u));
+  return r;
+}
+// The gated values of a piece.  low, top: per half the largest magnitude of the smaller candidates and of the larger ones.
 template <int P, int kType>
-__device__ __forceinline__ void gate_piece(QuantRow<P, kType>& r, int p, const uint4& ra, const uint4& rb, uint32_t& top) {
+__device__ __forceinline__ void gate_piece(QuantRow<P, kType>& r, int p, const uint4& ra, const uint4& rb, uint32_t& low, uint32_t& top) {
   float a[kPiece], b[kPiece];
   unpack_piece<kType>(ra, a);
   unpack_piece<kType>(rb, b);
@@ -474,18 +487,19 @@ __device__ __forceinline__ void gate_piece(QuantRow<P, kType>& r, int p, const u
 #pragma unroll
   for (int k = 1; k + 1 < kPiece; k += 2) least = min3(least, a[k], a[k + 1]);
   least = fminf(least, a[kPiece - 1]);
+  const float band = gated_band(least);
 #pragma unroll
-  for (int k = 0; k < kPiece / 2; ++k) gated_two<kType>(a[2 * k], a[2 * k + 1], b[2 * k], b[2 * k + 1], lo[k], hi[k]);
+  for (int k = 0; k < kPiece / 2; ++k) gated_two<kType>(a[2 * k], a[2 * k + 1], b[2 * k], b[2 * k + 1], band, lo[k], hi[k]);
   if (least < -80.0f) {
     const uint4 e = gated_exact_piece<kType>(ra, rb);
     lo[0] = hi[0] = e.x; lo[1] = hi[1] = e.y; lo[2] = hi[2] = e.z; lo[3] = hi[3] = e.w;
   }
 #pragma unroll
   for (int k = 0; k < kPiece / 2; ++k) {
-    const bool two = ((lo[k] ^ hi[k]) & 0x7FFF7FFFu) != 0u;      // (a zero's sign says nothing)
     r.h[p][k] = lo[k];
-    if (two) r.marks |= 1u << (4 * p + k);
-    top = max_halves(top, ((hi[k] << 1) & 0xFFFEFFFEu) | (two ? 0x00010001u : 0u));
+    r.marks[p / 4] += one_where_any((lo[k] ^ hi[k]) & 0x7FFF7FFFu) * (1u << (4 * (p & 3) + k));      // (a zero's sign says nothing)
+    low = max_magnitudes<kType>(low, lo[k]);
+    top = max_magnitudes<kType>(top, hi[k]);
   }
 }
 // fp32 bits of a 16-bit magnitude
@@ -521,7 +535,7 @@ quantize_i8_kernel(const QuantI8Args args) {
   };
   auto settle = [&](QuantRow<P, kType>& r, int p, float inverse, float largest) {
     if constexpr (kGated) {
-      const uint4 h = settle_piece<kType>(make_uint4(r.h[p][0], r.h[p][1], r.h[p][2], r.h[p][3]), r.marks >> (4 * p), row_x(row), row_x2(row), pl.at(p, 0), pl.at(0, 1) - pl.at(0, 0), args.m,
+      const uint4 h = settle_piece<kType>(make_uint4(r.h[p][0], r.h[p][1], r.h[p][2], r.h[p][3]), r.marks_of(p), row_x(row), row_x2(row), pl.at(p, 0), pl.at(0, 1) - pl.at(0, 0), args.m,
                                           inverse, largest);
       r.h[p][0] = h.x; r.h[p][1] = h.y; r.h[p][2] = h.z; r.h[p][3] = h.w;
     }
@@ -529,7 +543,10 @@ quantize_i8_kernel(const QuantI8Args args) {
   if (kAsync && row < rows) ask(row);
   for (; row < rows; row += stride, slot ^= 2) {
     QuantRow<P, kType> r;
-    r.marks = 0;
+    if constexpr (kGated) {
+#pragma unroll
+      for (int i = 0; i < (P + 3) / 4; ++i) r.marks[i] = 0;
+    }
     uint32_t bits;
     if constexpr (kAsync) copy_async_done();
     RawPiece<kType> raw[P], raw2[kGated && !kAsync ? P : 1];
@@ -548,33 +565,40 @@ quantize_i8_kernel(const QuantI8Args args) {
       }
       bits = row_max<kWarp>(max_bits<P>(r.v), sh, slot);
     } else {
-      uint32_t top = 0;
+      uint32_t top = 0, low = 0;
 #pragma unroll
       for (int p = 0; p < P; ++p) {
         if constexpr (kAsync) raw[p] = slot_raw<kType>(pl, p, slot_x);
         if constexpr (kGated) {
           if constexpr (kAsync) raw2[0] = slot_raw<kType>(pl, p, slot_x2);
-          gate_piece<P, kType>(r, p, raw[p].w[0], raw2[kAsync ? 0 : p].w[0], top);
+          gate_piece<P, kType>(r, p, raw[p].w[0], raw2[kAsync ? 0 : p].w[0], low, top);
         } else {
           r.h[p][0] = raw[p].w[0].x; r.h[p][1] = raw[p].w[0].y; r.h[p][2] = raw[p].w[0].z; r.h[p][3] = raw[p].w[0].w;
 #pragma unroll
-          for (int k = 0; k < kPiece / 2; ++k) top = max_halves(top, r.h[p][k] & 0x7FFF7FFFu);
+          for (int k = 0; k < kPiece / 2; ++k) top = max_magnitudes<kType>(top, r.h[p][k]);
         }
       }
-      uint32_t largest = row_max<kWarp>(max(top >> 16, top & 0xFFFFu), sh, slot);
+      uint32_t largest = max(top >> 16, top & 0xFFFFu);
       if constexpr (kGated) {
-        if (largest & 1u) {                         // the largest has two candidates (the same for every thread of the row)
+        // The largest of the larger candidates and, behind it, that of the smaller ones (of the threads that have the former): the same, or else the
+        // largest magnitude itself has two candidates.
+        largest = row_max<kWarp>((largest << 16) | max(low >> 16, low & 0xFFFFu), sh, slot);
+        const bool unsettled = (largest >> 16) != (largest & 0xFFFFu);      // (for every thread of the row alike)
+        largest >>= 16;
+        if (unsettled) {
           top = 0;
 #pragma unroll
           for (int p = 0; p < P; ++p) {
-            if ((r.marks >> (4 * p)) & 15u) settle(r, p, -1.0f, 0.0f);
+            if (r.marks_of(p)) settle(r, p, -1.0f, 0.0f);
 #pragma unroll
-            for (int k = 0; k < kPiece / 2; ++k) top = max_halves(top, r.h[p][k] & 0x7FFF7FFFu);
+            for (int k = 0; k < kPiece / 2; ++k) top = max_magnitudes<kType>(top, r.h[p][k]);
           }
-          r.marks = 0;
-          largest = 2u * row_max<kWarp>(max(top >> 16, top & 0xFFFFu), sh, slot + 1);
+#pragma unroll
+          for (int i = 0; i < (P + 3) / 4; ++i) r.marks[i] = 0;
+          largest = row_max<kWarp>(max(top >> 16, top & 0xFFFFu), sh, slot + 1);
         }
-        largest >>= 1;
+      } else {
+        largest = row_max<kWarp>(largest, sh, slot);
       }
       bits = magnitude_bits<kType>(largest);
     }
@@ -590,7 +614,7 @@ quantize_i8_kernel(const QuantI8Args args) {
         if (pl.at(p, 0) >= pl.m) break;
         float v[kPiece];
         unpack_piece<kType>(make_uint4(r.h[p][0], r.h[p][1], r.h[p][2], r.h[p][3]), v);
-        if (kGated && ((r.marks >> (4 * p)) & 15u)) {
+        if (kGated && r.marks_of(p)) {
           // only a value that lies within a step of the 16-bit type of a border needs to be settled: 2^-10 (fp16) or 2^-7 of it, and 2^-24 (fp16) where that is less
           constexpr float kStep = kType == STB_F16 ? 9.765625e-4f : 7.8125e-3f;
           float near = 0.0f;
@@ -630,8 +654,9 @@ quantize_i8_long_kernel(const QuantI8Args args) {
 #pragma unroll
       for (int k = 0; k < kPiece; k += 2) {
         uint32_t lo, hi;
-        gated_two<kType>(v[0][k], v[0][k + 1], b[k], b[k + 1], lo, hi);
-        if (lo != hi || fminf(v[0][k], v[0][k + 1]) < -80.0f) lo = gated_exact<kType>(v[0][k], v[0][k + 1], b[k], b[k + 1]);
+        const float least = fminf(v[0][k], v[0][k + 1]);
+        gated_two<kType>(v[0][k], v[0][k + 1], b[k], b[k + 1], gated_band(least), lo, hi);
+        if (lo != hi || least < -80.0f) lo = gated_exact<kType>(v[0][k], v[0][k + 1], b[k], b[k + 1]);
         unpack_two<kType>(lo, v[0][k], v[0][k + 1]);
       }
     }
