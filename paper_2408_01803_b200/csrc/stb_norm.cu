@@ -241,16 +241,20 @@ __device__ __forceinline__ void ask_row(const RowPlace<true>& pl, const void* ro
     if (parts == 2) copy_async16(dst + (uint32_t)pl.width * 16u, src + 16);
   }
 }
+// Zeros in the slots behind the row's end, which nothing is ever copied into (every row ends at the same place).
+template <int kAll, int P>
+__device__ __forceinline__ void clear_slots(const RowPlace<true>& pl, int dt, uint8_t* slots) {
+  const int parts = (kAll == kAnyType ? dt : kAll) == STB_F32 ? 2 : 1;
+  for (int p = 0; p < P; ++p)
+    for (int h = 0; h < parts; ++h)
+      if (pl.at(p, 0) >= pl.m) reinterpret_cast<uint4*>(slots)[(parts * p + h) * pl.width + pl.lane] = make_uint4(0u, 0u, 0u, 0u);
+}
 template <int kType>
 __device__ __forceinline__ RawPiece<kType> slot_raw(const RowPlace<true>& pl, int p, const uint8_t* slots) {
   constexpr int kParts = kType == STB_F32 ? 2 : 1;
   RawPiece<kType> r;
 #pragma unroll
-  for (int h = 0; h < kParts; ++h) {
-    const uint4 v = reinterpret_cast<const uint4*>(slots)[(kParts * p + h) * pl.width + pl.lane];      // (behind the row's end: whatever is there)
-    const bool in = pl.at(p, 0) < pl.m;
-    r.w[h] = make_uint4(in ? v.x : 0u, in ? v.y : 0u, in ? v.z : 0u, in ? v.w : 0u);
-  }
+  for (int h = 0; h < kParts; ++h) r.w[h] = reinterpret_cast<const uint4*>(slots)[(kParts * p + h) * pl.width + pl.lane];
   return r;
 }
 // f(p, values) for every piece in the slots
@@ -540,7 +544,11 @@ quantize_i8_kernel(const QuantI8Args args) {
       r.h[p][0] = h.x; r.h[p][1] = h.y; r.h[p][2] = h.z; r.h[p][3] = h.w;
     }
   };
-  if (kAsync && row < rows) ask(row);
+  if constexpr (kAsync) {
+    clear_slots<kType, P>(pl, kType, slot_x);
+    if (kGated) clear_slots<kType, P>(pl, kType, slot_x2);
+    if (row < rows) ask(row);
+  }
   for (; row < rows; row += stride, slot ^= 2) {
     QuantRow<P, kType> r;
     if constexpr (kGated) {
@@ -720,7 +728,11 @@ block_norm_kernel(const __grid_constant__ stb_norm a) {
       if (resid) ask_row<kAll, P>(pl, row_of(resid, r, a.ldr, a.rdt), a.rdt, slot_r);
     }
   };
-  if (kAsync && row < rows) ask(row);
+  if constexpr (kAsync) {
+    clear_slots<kAll, P>(pl, a.xdt, slot_x);
+    if (resid) clear_slots<kAll, P>(pl, a.rdt, slot_r);
+    if (row < rows) ask(row);
+  }
   for (; row < rows; row += stride, slot ^= 5) {
     // What is asked for before the first sum: the residual beside x, and the vectors, as far as registers hold them.
     constexpr bool kEarly = !kAsync && (kWarp || P <= 2), kAhead = kVec && !kAsync && (P == 1 || (P == 2 && kAll != kAnyType));
