@@ -289,7 +289,7 @@ int stb_allocate_nm(const double *sumsq, int layers, double r_target, int *N_out
  * token) and weights (a row is an output channel) alike.  A row without anything but zeros, or whose largest magnitude is below 2^-118,
  * becomes zeros with scale 0; one with an infinity or a NaN becomes zeros with scale NaN, so that every product with it is NaN.
  * x: [rows][ldx]; x2: [rows][ldx2]; q: [rows][ldq] (what lies behind the m-th value of a row is left as it is); leading dimensions >= m, in elements.  Any alignment
- * of x, x2 and q is taken; 16-byte rows (q: 8-byte) are the fast case.  One launch. */
+ * of x, x2 and q is taken; 16-byte rows (fp32: 32-byte, q: 8-byte) are the fast case.  One launch. */
 int stb_quantize_i8(const void *x, size_t ldx, const void *x2, size_t ldx2, stb_dtype xdt, int rows, int m, int8_t *q, size_t ldq,
                     float *scale, void *stream);
 
@@ -338,7 +338,7 @@ typedef struct stb_norm {
 
 /* Norms before and after a block, fused with its gate, residual scale and residual sum: one pass over the tokens, one launch.  An output
  * may be the input of its type with the same leading dimension (resid_out = resid, y = x); otherwise outputs must not overlap anything.
- * Any alignment is taken; 16-byte rows (q: 8-byte) are the fast case.  (Squares of values beyond 10^19 overflow fp32: such a token is 0 or NaN.) */
+ * Any alignment is taken; 16-byte rows (fp32: 32-byte, q: 8-byte) are the fast case.  (Squares of values beyond 10^19 overflow fp32: such a token is 0 or NaN.) */
 int stb_block_norm(const stb_norm *args, void *stream);
 
 /* Static string for a status code. */

@@ -88,8 +88,16 @@ __device__ __forceinline__ void unpack_piece(const uint4& a, float (&v)[kPiece])
   unpack_two<kType>(a.x, v[0], v[1]); unpack_two<kType>(a.y, v[2], v[3]);
   unpack_two<kType>(a.z, v[4], v[5]); unpack_two<kType>(a.w, v[6], v[7]);
 }
-// Eight values as they lie in memory: 16 bytes, fp32 twice that.
+// Eight values as they lie in memory: 16 bytes, fp32 twice that, which one instruction moves: two of 16 bytes would each touch half of every 32-byte sector.
 template <int kType> struct RawPiece { uint4 w[kType == STB_F32 ? 2 : 1]; };
+__device__ __forceinline__ void load_32(const void* p, uint4 (&w)[2]) {
+  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(w[0].x), "=r"(w[0].y), "=r"(w[0].z), "=r"(w[0].w), "=r"(w[1].x), "=r"(w[1].y), "=r"(w[1].z), "=r"(w[1].w) : "l"(p));
+}
+__device__ __forceinline__ void store_32(void* p, const float (&v)[kPiece]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
+}
 template <int kType>
 __device__ __forceinline__ void values_of(const RawPiece<kType>& r, float (&v)[kPiece]) {
   if constexpr (kType == STB_F32) {
@@ -112,9 +120,9 @@ __device__ __forceinline__ RawPiece<kType> load_piece(const RowPlace<kVec>& pl, 
   if constexpr (kVec) {
     const int i = pl.at(p, 0);
     if (i < pl.m) {
-      const uint4* q = reinterpret_cast<const uint4*>(static_cast<const char*>(row) + (size_t)i * (2 * kParts));
-#pragma unroll
-      for (int h = 0; h < kParts; ++h) r.w[h] = q[h];
+      const char* q = static_cast<const char*>(row) + (size_t)i * (2 * kParts);
+      if constexpr (kType == STB_F32) load_32(q, r.w);
+      else r.w[0] = *reinterpret_cast<const uint4*>(q);
     }
   } else {
     uint32_t u[kPiece];
@@ -197,8 +205,7 @@ __device__ __forceinline__ void store_row(const RowPlace<kVec>& pl, void* row, i
       if constexpr (kType == STB_F32) {
         float* q = static_cast<float*>(row);
         if (kVec) {
-          reinterpret_cast<float4*>(q + i)[0] = make_float4(v[p][0], v[p][1], v[p][2], v[p][3]);
-          reinterpret_cast<float4*>(q + i)[1] = make_float4(v[p][4], v[p][5], v[p][6], v[p][7]);
+          store_32(q + i, v[p]);
         } else {
 #pragma unroll
           for (int k = 0; k < kPiece; ++k)
@@ -222,23 +229,37 @@ __device__ __forceinline__ void store_row(const RowPlace<kVec>& pl, void* row, i
 }
 
 // ---- pieces on their way -----------------------------------------------------------------------------------------------------------
-// A row's pieces of a thread in shared memory: 16-byte part j of piece p at (parts p + j) width + lane, parts = 1 or, fp32, 2.
+// A row's pieces in shared memory, in their order: 16-byte part j of piece p of a thread at parts (p width + lane) + j, parts = 1 or, fp32, 2.  Pieces of one
+// part a thread copies for itself; those of two the threads of a warp copy for each other, neighbours side by side (each for itself they would take every
+// 32-byte sector twice: 4096 x 8192 fp32 in 8 bits @@ us), and the warp waits for all of its threads' copies.
 __device__ __forceinline__ void copy_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
-__device__ __forceinline__ void copy_async_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+__device__ __forceinline__ void copy_async_done() {
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncwarp();
+}
 template <int kAll, int P>
 __device__ __forceinline__ void ask_row(const RowPlace<true>& pl, const void* row, int dt, uint8_t* at) {
   const uint32_t slots = smem_u32(at);
-  const int parts = (kAll == kAnyType ? dt : kAll) == STB_F32 ? 2 : 1;
+  if ((kAll == kAnyType ? dt : kAll) == STB_F32) {
+    __syncwarp();                                   // (the neighbour has read its slots)
+    const int lane = pl.lane & 31, first = 2 * (pl.lane - lane) + lane;
 #pragma unroll
-  for (int p = 0; p < P; ++p) {
-    const int i = pl.at(p, 0);
-    if (i >= pl.m) break;
-    const char* src = static_cast<const char*>(row) + (size_t)i * (8 * parts / 4);
-    const uint32_t dst = slots + (uint32_t)((parts * p) * pl.width + pl.lane) * 16u;
-    copy_async16(dst, src);
-    if (parts == 2) copy_async16(dst + (uint32_t)pl.width * 16u, src + 16);
+    for (int p = 0; p < P; ++p) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int part = 2 * p * pl.width + first + 32 * h;
+        if (part * 4 < pl.m) copy_async16(slots + (uint32_t)part * 16u, static_cast<const char*>(row) + (size_t)part * 16);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      const int i = pl.at(p, 0);
+      if (i >= pl.m) break;
+      copy_async16(slots + (uint32_t)(p * pl.width + pl.lane) * 16u, static_cast<const char*>(row) + (size_t)i * 2);
+    }
   }
 }
 // Zeros in the slots behind the row's end, which nothing is ever copied into (every row ends at the same place).
@@ -247,14 +268,14 @@ __device__ __forceinline__ void clear_slots(const RowPlace<true>& pl, int dt, ui
   const int parts = (kAll == kAnyType ? dt : kAll) == STB_F32 ? 2 : 1;
   for (int p = 0; p < P; ++p)
     for (int h = 0; h < parts; ++h)
-      if (pl.at(p, 0) >= pl.m) reinterpret_cast<uint4*>(slots)[(parts * p + h) * pl.width + pl.lane] = make_uint4(0u, 0u, 0u, 0u);
+      if (pl.at(p, 0) >= pl.m) reinterpret_cast<uint4*>(slots)[parts * (p * pl.width + pl.lane) + h] = make_uint4(0u, 0u, 0u, 0u);
 }
 template <int kType>
 __device__ __forceinline__ RawPiece<kType> slot_raw(const RowPlace<true>& pl, int p, const uint8_t* slots) {
   constexpr int kParts = kType == STB_F32 ? 2 : 1;
   RawPiece<kType> r;
 #pragma unroll
-  for (int h = 0; h < kParts; ++h) r.w[h] = reinterpret_cast<const uint4*>(slots)[(kParts * p + h) * pl.width + pl.lane];
+  for (int h = 0; h < kParts; ++h) r.w[h] = reinterpret_cast<const uint4*>(slots)[kParts * (p * pl.width + pl.lane) + h];
   return r;
 }
 // f(p, values) for every piece in the slots
@@ -865,6 +886,7 @@ static RowShape row_shape(int m, int rows, bool vec, const RowNeeds& need) {
   return s;
 }
 
+// a piece's bytes: 8 bits 8, 16 bits 16, fp32 32
 static bool rows_aligned(const void* p, size_t ld, int bytes, size_t to) { return !p || ((reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0 && (ld * (size_t)bytes) % to == 0); }
 static bool element_aligned(const void* p, int dt) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(dtype_bytes(dt) - 1)) == 0; }
 static bool known_dtype(int dt) { return dt == STB_F16 || dt == STB_BF16 || dt == STB_F32; }
@@ -937,7 +959,7 @@ extern "C" int stb_quantize_i8(const void* x, size_t ldx, const void* x2, size_t
   if (ldx < (size_t)m || (x2 && ldx2 < (size_t)m) || ldq < (size_t)m) return STB_ERR_ARG;
   if (!stb::element_aligned(x, xdt) || !stb::element_aligned(x2, xdt) || !stb::element_aligned(scale, STB_F32)) return STB_ERR_ARG;
   const int bytes = stb::dtype_bytes(xdt);
-  const bool vec = m % stb::kPiece == 0 && stb::rows_aligned(x, ldx, bytes, 16) && stb::rows_aligned(x2, ldx2, bytes, 16) && stb::rows_aligned(q, ldq, 1, 8);
+  const bool vec = m % stb::kPiece == 0 && stb::rows_aligned(x, ldx, bytes, 8 * bytes) && stb::rows_aligned(x2, ldx2, bytes, 16) && stb::rows_aligned(q, ldq, 1, 8);
   const stb::QuantI8Args a = {x, x2, rows, m, ldx, ldx2, ldq, q, scale};
   const stb::RowShape s = stb::row_shape(m, rows, vec, {xdt == STB_F32 || x2 ? 32u : 16u, 4u * 128u, 1024, x2 ? 0 : (xdt == STB_F32 ? 512 : 1024), x2 ? 1024 : 512, 4});
   cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -969,10 +991,10 @@ extern "C" int stb_block_norm(const stb_norm* args, void* stream) {
       !stb::element_aligned(a.gate, a.wdt) || !stb::element_aligned(a.weight, a.wdt) || !stb::element_aligned(a.bias, a.wdt))
     return STB_ERR_ARG;
   const int xb = stb::dtype_bytes(a.xdt), rb = stb::dtype_bytes(a.rdt), wb = stb::dtype_bytes(a.wdt), yb = stb::dtype_bytes(a.ydt);
-  const bool vec = a.h % stb::kPiece == 0 && stb::rows_aligned(a.x, a.ldx, xb, 16) && stb::rows_aligned(a.resid, a.ldr, rb, 16) && stb::rows_aligned(a.resid_out, a.ldro, rb, 16) &&
-                   stb::rows_aligned(a.y, a.ldy, yb, 16) && stb::rows_aligned(a.q, a.ldq, 1, 8) && stb::rows_aligned(a.gate, a.tokens > a.tokens_per_gate ? a.ldgate : 0, wb, 16) &&
-                   stb::rows_aligned(a.post_weight, 0, wb, 16) && stb::rows_aligned(a.post_bias, 0, wb, 16) && stb::rows_aligned(a.weight, 0, wb, 16) &&
-                   stb::rows_aligned(a.bias, 0, wb, 16);
+  const bool vec = a.h % stb::kPiece == 0 && stb::rows_aligned(a.x, a.ldx, xb, 8 * xb) && stb::rows_aligned(a.resid, a.ldr, rb, 8 * rb) && stb::rows_aligned(a.resid_out, a.ldro, rb, 8 * rb) &&
+                   stb::rows_aligned(a.y, a.ldy, yb, 8 * yb) && stb::rows_aligned(a.q, a.ldq, 1, 8) && stb::rows_aligned(a.gate, a.tokens > a.tokens_per_gate ? a.ldgate : 0, wb, 8 * wb) &&
+                   stb::rows_aligned(a.post_weight, 0, wb, 8 * wb) && stb::rows_aligned(a.post_bias, 0, wb, 8 * wb) && stb::rows_aligned(a.weight, 0, wb, 8 * wb) &&
+                   stb::rows_aligned(a.bias, 0, wb, 8 * wb);
   const bool same = a.xdt != STB_F32 && (!residual || a.rdt == a.xdt) && (!vectors || a.wdt == a.xdt);
   const uint32_t each = (a.xdt == STB_F32 ? 32u : 16u) + (!a.resid ? 0u : (a.rdt == STB_F32 ? 32u : 16u));
   const stb::RowShape s = stb::row_shape(a.h, a.tokens, vec, {each, 10u * 128u, 1024, 512, 512, 2});
