@@ -150,7 +150,7 @@ template <int kAll, int P, bool kVec, class F>
 __device__ __forceinline__ void for_row(const RowPlace<kVec>& pl, const void* row, int dt, F f) {
   by_type<kAll>(dt, [&](auto type) {
     constexpr int kType = decltype(type)::value;
-    constexpr int kAtOnce = P <= 2 ? P : (!kVec || kType == STB_F32 ? 2 : P);      // (registers)
+    constexpr int kAtOnce = P <= 2 ? P : (!kVec || kType == STB_F32 ? 2 : (kAll == kAnyType ? 4 : P));      // (registers)
 #pragma unroll
     for (int p0 = 0; p0 < P; p0 += kAtOnce) {
       RawPiece<kType> raw[kAtOnce];
@@ -730,7 +730,7 @@ __device__ __forceinline__ void norm_row(const RowPlace<kVec>& pl, float (&v)[P]
 }
 // kAll: the type of x, the residual and the weights, where it is the same 16-bit type.
 template <int kAll, int P, bool kVec, bool kWarp, bool kAsync>
-__global__ void __launch_bounds__(kWarp ? 256 : (kAsync || (!kVec && P > 2) ? 512 : kMaxRowThreads), kWarp || (kAsync && P <= 4) ? 2 : 1)
+__global__ void __launch_bounds__(kWarp ? 256 : (kAsync && P <= 4 && kAll == kAnyType ? 768 : (kAsync || (!kVec && P > 2) ? 512 : kMaxRowThreads)), kWarp || (kAsync && P <= 4 && kAll != kAnyType) ? 2 : 1)
 block_norm_kernel(const __grid_constant__ stb_norm a) {
   extern __shared__ __align__(16) uint8_t slots[];
   __shared__ float sh[10][32];                      // the parts of a row's five reductions, and of the next one's
@@ -997,7 +997,7 @@ extern "C" int stb_block_norm(const stb_norm* args, void* stream) {
                    stb::rows_aligned(a.bias, 0, wb, 8 * wb);
   const bool same = a.xdt != STB_F32 && (!residual || a.rdt == a.xdt) && (!vectors || a.wdt == a.xdt);
   const uint32_t each = (a.xdt == STB_F32 ? 32u : 16u) + (!a.resid ? 0u : (a.rdt == STB_F32 ? 32u : 16u));
-  const stb::RowShape s = stb::row_shape(a.h, a.tokens, vec, {each, 10u * 128u, 1024, 512, 512, 2});
+  const stb::RowShape s = stb::row_shape(a.h, a.tokens, vec, {each, 10u * 128u, same ? 1024 : 768, 512, same ? 512 : 768, 2});
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const cudaError_t e = !same ? stb::launch_norm<stb::kAnyType>(a, s, vec, st) : (a.xdt == STB_F16 ? stb::launch_norm<STB_F16>(a, s, vec, st) : stb::launch_norm<STB_BF16>(a, s, vec, st));
   return e == cudaSuccess ? STB_OK : STB_ERR_CUDA;
