@@ -728,9 +728,10 @@ __device__ __forceinline__ void norm_row(const RowPlace<kVec>& pl, float (&v)[P]
 #pragma unroll
     for (int k = 0; k < kPiece; k += 2) mul_two(v[p][k], v[p][k + 1], v[p][k], v[p][k + 1], inv, inv);
 }
-// kAll: the type of x, the residual and the weights, where it is the same 16-bit type.
-template <int kAll, int P, bool kVec, bool kWarp, bool kAsync>
-__global__ void __launch_bounds__(kWarp ? 256 : (kAsync && P <= 4 && kAll == kAnyType ? 768 : (kAsync || (!kVec && P > 2) ? 512 : kMaxRowThreads)), kWarp || (kAsync && P <= 4 && kAll != kAnyType) ? 2 : 1)
+// kAll: the type of x, the residual and the weights, where it is the same 16-bit type.  kRoomy (kAsync, four pieces): 80 registers a thread, of which 768 fit an
+// SM, instead of 64 and 1024.
+template <int kAll, int P, bool kVec, bool kWarp, bool kAsync, bool kRoomy = false>
+__global__ void __launch_bounds__(kWarp ? 256 : (kRoomy ? 768 : (kAsync || (!kVec && P > 2) ? 512 : kMaxRowThreads)), kWarp || (kAsync && P <= 4 && !kRoomy) ? 2 : 1)
 block_norm_kernel(const __grid_constant__ stb_norm a) {
   extern __shared__ __align__(16) uint8_t slots[];
   __shared__ float sh[10][32];                      // the parts of a row's five reductions, and of the next one's
@@ -932,21 +933,33 @@ static cudaError_t launch_quantize(const QuantI8Args& a, const RowShape& s, bool
   return vec ? launch_quantize_as<kType, kGated, true>(a, s, st) : launch_quantize_as<kType, kGated, false>(a, s, st);
 }
 template <int kAll, bool kVec>
-static cudaError_t launch_norm_as(const stb_norm& a, const RowShape& s, cudaStream_t st) {
+static cudaError_t launch_norm_as(const stb_norm& a, const RowShape& s, bool roomy, cudaStream_t st) {
   if (s.warp) {
     if (s.pieces == 1) return launch_rows<block_norm_kernel<kAll, 1, kVec, true, false>>(s, st, a);
     return s.pieces == 2 ? launch_rows<block_norm_kernel<kAll, 2, kVec, true, false>>(s, st, a) : launch_rows<block_norm_kernel<kAll, 4, kVec, true, false>>(s, st, a);
   }
   if constexpr (kVec) {
-    if (s.slots) return s.pieces == 4 ? launch_rows<block_norm_kernel<kAll, 4, true, false, true>>(s, st, a) : launch_rows<block_norm_kernel<kAll, 8, true, false, true>>(s, st, a);
+    if (s.slots && s.pieces == 8) return launch_rows<block_norm_kernel<kAll, 8, true, false, true>>(s, st, a);
+    if constexpr (kAll != kAnyType) {
+      if (s.slots && !roomy) return launch_rows<block_norm_kernel<kAll, 4, true, false, true>>(s, st, a);
+    }
+    if (s.slots) return launch_rows<block_norm_kernel<kAll, 4, true, false, true, true>>(s, st, a);
   }
   if (s.pieces == 1) return launch_rows<block_norm_kernel<kAll, 1, kVec, false, false>>(s, st, a);
   if (s.pieces == 2) return launch_rows<block_norm_kernel<kAll, 2, kVec, false, false>>(s, st, a);
   return launch_rows<block_norm_kernel<kAll, kVec ? 4 : 8, kVec, false, false>>(s, st, a);
 }
 template <int kAll>
-static cudaError_t launch_norm(const stb_norm& a, const RowShape& s, bool vec, cudaStream_t st) {
-  return vec ? launch_norm_as<kAll, true>(a, s, st) : launch_norm_as<kAll, false>(a, s, st);
+static cudaError_t launch_norm(const stb_norm& a, const RowShape& s, bool vec, bool roomy, cudaStream_t st) {
+  return vec ? launch_norm_as<kAll, true>(a, s, roomy, st) : launch_norm_as<kAll, false>(a, s, roomy, st);
+}
+// Whether the norms of rows on their way take 80 registers a thread (nothing is then spilled) or 64 (more rows at a time).  Tokens of mixed types: always
+// (2048 x 4096 with an fp32 residual 16.3 us against 19.0; 11008, layer norm with fp32 weights, 45 against 56; but 16384 77 against 70).  Of one type: where
+// more than three quarters as many threads fit an SM (2048 x 2816 8.1 us against 9.5, 22016 57.9 against 60.1, but 5120 14.2 against 13.0), or, with the norm
+// before the gate, as many as that (8192 27.6 against 28.2).
+static bool norm_roomy(int h, bool same, bool post) {
+  const int threads = ((h + 4 * kPiece - 1) / (4 * kPiece) + 31) / 32 * 32, most = threads <= 512 ? 1024 / threads * threads : 0, roomy = threads <= 768 ? 768 / threads * threads : 0;
+  return !same || 4 * roomy > 3 * most || (post && 4 * roomy == 3 * most);
 }
 
 }  // namespace stb
@@ -997,8 +1010,9 @@ extern "C" int stb_block_norm(const stb_norm* args, void* stream) {
                    stb::rows_aligned(a.bias, 0, wb, 8 * wb);
   const bool same = a.xdt != STB_F32 && (!residual || a.rdt == a.xdt) && (!vectors || a.wdt == a.xdt);
   const uint32_t each = (a.xdt == STB_F32 ? 32u : 16u) + (!a.resid ? 0u : (a.rdt == STB_F32 ? 32u : 16u));
-  const stb::RowShape s = stb::row_shape(a.h, a.tokens, vec, {each, 10u * 128u, same ? 1024 : 768, 512, same ? 512 : 768, 2});
+  const bool roomy = stb::norm_roomy(a.h, same, a.post != 0);
+  const stb::RowShape s = stb::row_shape(a.h, a.tokens, vec, {each, 10u * 128u, roomy ? 768 : 1024, 512, roomy ? 768 : 512, 2});
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = !same ? stb::launch_norm<stb::kAnyType>(a, s, vec, st) : (a.xdt == STB_F16 ? stb::launch_norm<STB_F16>(a, s, vec, st) : stb::launch_norm<STB_BF16>(a, s, vec, st));
+  const cudaError_t e = !same ? stb::launch_norm<stb::kAnyType>(a, s, vec, roomy, st) : (a.xdt == STB_F16 ? stb::launch_norm<STB_F16>(a, s, vec, roomy, st) : stb::launch_norm<STB_BF16>(a, s, vec, roomy, st));
   return e == cudaSuccess ? STB_OK : STB_ERR_CUDA;
 }
