@@ -483,6 +483,31 @@ def test_norm_parts(stb, T, h):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("h", (1032, 2816, 5120, 8192, 11008, 16384, 17000, 24576, 24584, 28672, 32768))
+def test_norms_of_many_tokens(stb, h):
+    """More tokens than CTAs stay on the GPU: the next one's values on their way, in every form that takes them."""
+    T = max(310, min(1500, 5_000_000 // h))
+    f32 = dict(x="f32", r="f32", w="f32", y="f32")
+    for k, kw in enumerate((dict(r="f32"), dict(y="i8"), dict(x="bf16", r="bf16", w="bf16", y="bf16", post=True, post_w=True, gate=1, alpha=0.5),
+                            dict(kind="layer", w="f32", bias=True, inplace=True, place=(16, 8)), f32 if h <= 28672 else dict(r=None))):
+        _check_norm(stb, T, h, 17 * h + k, **kw)
+
+
+@pytest.mark.gpu
+def test_rows_of_fp32_off_their_pieces(stb):
+    """fp32 rows on 16-byte boundaries that are on no 32-byte ones."""
+    for T, h in ((3, 4096), (400, 1032)):
+        buf = torch.randn(T, h + 12, generator=_gen(h), dtype=torch.float32).cuda()
+        for x in (buf[:, 4:h + 4], buf.view(-1)[4:4 + T * h].view(T, h)):
+            q, s = stb.quantize_i8(x)
+            _check_rows(q, s, x.cpu())
+            w = torch.randn(h + 4, generator=_gen(T)).cuda()[4:]
+            y, _ = stb.block_norm(x, w)
+            want_y, _, ey, _ = _block64(x.cpu(), w.cpu(), None, None, False, None, None, None, 1.0, "rms", 1e-5)
+            assert ((y.cpu().double() - want_y).abs() <= 1.001 * (ey + U32 * want_y.abs())).all()
+
+
+@pytest.mark.gpu
 def test_norm_of_nothing_and_of_no_numbers(stb):
     for h in (50, 1500):
         x = _values(6, h, 3)
