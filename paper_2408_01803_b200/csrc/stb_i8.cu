@@ -204,7 +204,8 @@ __device__ __forceinline__ void i8_channel_out(const I8Args& a, const uint32_t (
 // Some tokens (a decode batch, a short prompt): one CTA per 128 channels, `bn` tokens and part of K; the `ks` parts of a tile are a cluster.
 //   warp 0 brings the stages by TMA, warp 1 issues the products (it also owns tensor memory); then all eight warps read the sums out.
 // ks = 1: straight to Y.  Else eight tokens at a time belong to one CTA of the cluster (group of eight mod ks), which gets everybody's sums of them
-// into its shared memory (32 bytes per channel and CTA), adds, scales and stores.
+// into its shared memory (32 bytes per channel and CTA), adds, scales and stores.  Bound by HBM where W is large (28672 x 8192, one token 38.7 us, 94 % of its
+// bytes' time; 4096 x 11008, 64 tokens, 11.1 us: 64 %, the rest the way from the launch to the first stage and the sum of the cluster).
 struct I8Batch { int lks, per, stages, ttiles, bn, ring, prefetch; uint32_t stage_bytes, tmem; };
 constexpr int kI8BatchThreads = 256;
 constexpr uint32_t kI8BatchScale = 1024, kI8BatchRing = 2048;     // the tokens' scales; the ring, and behind it the sums that the CTAs hand over
@@ -464,7 +465,8 @@ static int launch_i8_batch(const I8Args& a, const I8Plan& plan, int* dev_status,
 // rows, the first one's issuing lane multiplies for both, and each has the sums of its 128 channels for all tokens in its tensor memory.  The
 // clusters stay for the whole call and take every so-many-th tile (tokens fastest, so that W is read from HBM once); two accumulators of 256 columns,
 // so that a tile is read out while the next one is multiplied.  Per 128 columns of K a CTA fetches 16 KB + bn / 2 rows for 256 x bn x 128
-// multiply-adds of the pair: at bn = 256 64 bytes per clock of the tensor core, what an SM gets from L2.
+// multiply-adds of the pair: at bn = 256 64 bytes per clock of the tensor core, what an SM gets from L2.  28672 x 8192, 2048 tokens, 282 us: 3.4 POP/s (3.0 once the
+// GPU is at its power limit).
 //   warp 0 brings the stages, warp 1 issues the products, warps 4 to 7 read the sums out: 32 tokens at a time through shared memory, from where they leave
 //   as rows of 128 channels by TMA (or by plain stores where rows of Y are on no 16-byte boundary).
 struct I8Prefill { int stages, ttiles, tiles, bn, ring, tma_out; uint32_t stage_bytes; };
