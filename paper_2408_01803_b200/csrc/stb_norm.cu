@@ -150,7 +150,7 @@ template <int kAll, int P, bool kVec, class F>
 __device__ __forceinline__ void for_row(const RowPlace<kVec>& pl, const void* row, int dt, F f) {
   by_type<kAll>(dt, [&](auto type) {
     constexpr int kType = decltype(type)::value;
-    constexpr int kAtOnce = P <= 2 ? P : (!kVec || kType == STB_F32 ? 2 : (kAll == kAnyType ? 4 : P));      // (registers)
+    constexpr int kAtOnce = P <= 2 ? P : (!kVec || kType == STB_F32 ? 2 : P);      // (registers)
 #pragma unroll
     for (int p0 = 0; p0 < P; p0 += kAtOnce) {
       RawPiece<kType> raw[kAtOnce];
