@@ -625,17 +625,17 @@ gemm_i8_prefill_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_co
       for (int i = t128; i < sh.bn; i += 128) scales[i] = tok0 + i < args.T ? x_scale[tok0 + i] : 0.0f;
       if (!barrier_and(gemm_wait(bar_acc_full + 8 * acc, (uint32_t)(use >> 1) & 1u, abort_flag))) break;      // (one verdict for the four warps)
       tc_fence_after();
-      uint32_t v[2][32];
+      uint32_t even[32], odd[32];
       const uint32_t from = tmem_d + ((uint32_t)(32 * q) << 16) + 256u * acc;
-      tmem_ask32(from, v[0]);
-#pragma unroll 2
-      for (int c0 = 0; c0 < sh.bn; c0 += kI8OutTokens, buf ^= 1) {
-        uint32_t(&now)[32] = v[(c0 / kI8OutTokens) & 1];
+      // Only chunks that hold a result are read and written, none where all 128 channels lie behind n.  Every chunk therefore leaves one store, so that "all but the
+      // newest store" is every use of the buffer that a chunk takes: the buffers alternate with the stores, from tile to tile too.
+      const int live = r0 < args.n ? min(sh.bn, args.T - tok0) : 0;
+      auto chunk = [&](int c0, uint32_t (&now)[32], uint32_t (&next)[32]) {
         tmem_wait32(now);
-        if (c0 + kI8OutTokens < sh.bn) tmem_ask32(from + (uint32_t)(c0 + kI8OutTokens), v[((c0 / kI8OutTokens) & 1) ^ 1]);
+        if (c0 + kI8OutTokens < live) tmem_ask32(from + (uint32_t)(c0 + kI8OutTokens), next);
         const uint32_t out = sbase + kI8PrefillOut + (uint32_t)buf * kI8OutBytes;
-        if (t128 == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");       // the store before last has read this buffer
-        asm volatile("bar.sync 1, 128;" ::: "memory");
+        if (t128 == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");       // the store before last, this buffer's, has read it
+        asm volatile("bar.sync 1, 128;" ::: "memory");             // (plain stores: each thread reads back what it alone has written)
         switch (args.ydt) {
           case STB_F32: i8_rows_out<STB_F32>(now, scales + c0, ws, b, bias != nullptr, out, row); break;
           case STB_F16: i8_rows_out<STB_F16>(now, scales + c0, ws, b, bias != nullptr, out, row); break;
@@ -643,20 +643,25 @@ gemm_i8_prefill_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_co
         }
         if (sh.tma_out) fence_async_smem();
         asm volatile("bar.sync 1, 128;" ::: "memory");
-        if (r0 >= args.n || tok0 + c0 >= args.T) continue;
         if (sh.tma_out) {
           if (t128 == 0) {
             asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(&ymap), "r"(out), "r"(r0), "r"(tok0 + c0) : "memory");
             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
           }
         } else if (r < args.n) {
-          for (int i = 0; i < kI8OutTokens && tok0 + c0 + i < args.T; ++i) {
+          for (int i = 0; i < kI8OutTokens && c0 + i < live; ++i) {
             const size_t at = (size_t)(tok0 + c0 + i) * args.ldy + r;
             const uint8_t* p = smem + kI8PrefillOut + (size_t)buf * kI8OutBytes + (size_t)(i * kI8M + row) * elem;
             if (elem == 4) static_cast<float*>(args.Y)[at] = *reinterpret_cast<const float*>(p);
             else static_cast<uint16_t*>(args.Y)[at] = *reinterpret_cast<const uint16_t*>(p);
           }
         }
+        buf ^= 1;
+      };
+      if (live > 0) tmem_ask32(from, even);
+      for (int c0 = 0; c0 < live; c0 += 2 * kI8OutTokens) {
+        chunk(c0, even, odd);
+        if (c0 + kI8OutTokens < live) chunk(c0 + kI8OutTokens, odd, even);
       }
       tc_fence_before();
       __syncwarp();
