@@ -76,6 +76,30 @@ def test_product_of_many_tokens(stb, shape):
             calls = [stb.gemm_i8(xq, xs, wq, ws, bias=b, out_dtype=t) for _ in range(4)]
             for got in calls:
                 assert _same(got, want), (shape, t, b is not None)
+            # rows of a larger buffer: on 16-byte boundaries, and on none
+            for pad, shift in ((32, 16), (-n % 2 + 5, 3)):
+                ld = n + pad - (n % 16 if pad == 32 else 0)
+                buf = torch.full((T * ld + 32,), 7.0, dtype=t, device="cuda")
+                y = buf[shift:shift + T * ld].view(T, ld)[:, :n]
+                stb.gemm_i8(xq, xs, wq, ws, bias=b, out=y)
+                assert _same(y, want), (shape, t, b is not None, pad)
+                y.fill_(7.0)
+                assert bool((buf == 7.0).all()), (shape, t, "around the result")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", (1, 3, 7, 9, 130, 257, 263))
+def test_few_channels_of_many_tokens_in_wider_rows(stb, n):
+    """What lies beside the result in its rows stays as it is, wherever the last channel lies in a 16-byte piece."""
+    m, T = 128, 1025
+    xq, xs = _eight(T, m, n)
+    wq, ws = _eight(n, m, n + 1)
+    y32 = torch.round(xq.double() @ wq.double().T).float().mul_(xs[:, None]).mul_(ws)
+    for t in (torch.float32, torch.float16, torch.bfloat16):
+        buf = torch.full((T, 288), 7.0, dtype=t, device="cuda")
+        stb.gemm_i8(xq, xs, wq, ws, out=buf[:, 16:16 + n])
+        assert torch.equal(buf[:, 16:16 + n], y32.to(t))
+        assert bool((buf[:, :16] == 7.0).all()) and bool((buf[:, 16 + n:] == 7.0).all()), t
 
 
 @pytest.mark.gpu
