@@ -297,9 +297,16 @@ int stb_quantize_i8(const void *x, size_t ldx, const void *x2, size_t ldx2, stb_
  * STB_ERR_SHAPE), rounded to fp32, multiplied by x_scale[t], then by w_scale[i], then the bias is added, each in fp32, and the result is rounded
  * once to Y's type: every form of the kernel gives the same bits.  W: int8 [n][ldw], X: int8 [T][ldx]; n, T of 1 to 2^30; ldw, ldx >= m
  * and multiples of 16, W and X 16-byte aligned (what lies behind the m-th value of a row is not read into the result); w_scale: fp32 [n],
- * x_scale: fp32 [T], bias: fp32 [n] or NULL; Y: fp32, fp16 or bf16 [T][ldy], ldy >= n.  No workspace.  dev_status: as for stb_gemm. */
+ * x_scale: fp32 [T], bias: fp32 [n] or NULL; Y: fp32, fp16 or bf16 [T][ldy], ldy >= n (what lies behind the n-th value of a row is left as it is).  No workspace.
+ * dev_status: as for stb_gemm.  With or without it, results that a bounded wait which ran out kept from being computed are NaN. */
 int stb_gemm_i8(const int8_t *W, size_t ldw, const float *w_scale, const float *bias, int n, int m, const int8_t *X, size_t ldx,
                 const float *x_scale, int T, void *Y, stb_dtype ydt, size_t ldy, int *dev_status, void *stream);
+
+/* Self-test of its bounded waits, in the manner of stb_gemv_wait_selftest: the last part of K (one token to hundreds) or every tile of a CTA pair but its first (many
+ * tokens) is not copied, the limit is about 50 microseconds.  *dev_status (required) becomes STB_ERR_TIMEOUT; results without that part are NaN, the others are right.
+ * Sizes whose kernel has no such wait (few tokens and weights) give STB_ERR_UNSUPPORTED. */
+int stb_gemm_i8_wait_selftest(const int8_t *W, size_t ldw, const float *w_scale, const float *bias, int n, int m, const int8_t *X, size_t ldx,
+                              const float *x_scale, int T, void *Y, stb_dtype ydt, size_t ldy, int *dev_status, void *stream);
 
 typedef enum stb_norm_kind {
   STB_NORM_RMS = 0,         /* norm(v) = v / sqrt(mean_j v_j^2 + eps) */

@@ -27,7 +27,7 @@ EXPORTS = ["stb_pack_size", "stb_pack", "stb_packed_info", "stb_dequant", "stb_g
            "stb_gemm_workspace", "stb_gemm_workspace_min", "stb_gemm", "stb_gemm_f16_workspace", "stb_gemm_f16", "stb_gemm_noalloc", "stb_layer_stack", "stb_layer_stack_host",
            "stb_layer_stack_resident_workspace", "stb_layer_stack_resident", "stb_layer_stack_resident_host",
            "stb_layer_stack_resident_wait_selftest", "stb_layer_stack_checksum", "stb_quantize_workspace", "stb_quantize", "stb_weight_sumsq",
-           "stb_allocate_nm", "stb_quantize_i8", "stb_gemm_i8", "stb_block_norm", "stb_status_str"]
+           "stb_allocate_nm", "stb_quantize_i8", "stb_gemm_i8", "stb_gemm_i8_wait_selftest", "stb_block_norm", "stb_status_str"]
 
 
 class StbError(RuntimeError):
@@ -93,6 +93,7 @@ def _load():
     lib.stb_allocate_nm.argtypes = [p(C.c_double), i, C.c_double, p(i)]
     lib.stb_quantize_i8.argtypes = [v, z, v, z, i, i, i, v, z, v, v]
     lib.stb_gemm_i8.argtypes = [v, z, v, v, i, i, v, z, v, i, v, i, z, v, v]
+    lib.stb_gemm_i8_wait_selftest.argtypes = lib.stb_gemm_i8.argtypes
     lib.stb_block_norm.argtypes = [p(_Norm), v]
     lib.stb_status_str.argtypes = [i]
     lib.stb_status_str.restype = C.c_char_p
@@ -564,11 +565,18 @@ def _quantize_i8_py(x, x2=None, q=None, scale=None, stream=None):
 def gemm_i8(xq, x_scale, wq, w_scale, bias=None, out=None, out_dtype=None, dev_status=None, stream=None):
     """stb_gemm_i8: the linear layer in 8 bits, y[t][i] = x_scale[t] w_scale[i] sum_j wq[i][j] xq[t][j] (+ bias[i]), from one token to
     thousands.  xq: int8 [T][m] (or one token), wq: int8 [n][m], both on row strides of whole 16 bytes, as quantize_i8() makes them;
-    scales and bias fp32; y fp32 (default), fp16 or bf16 [T][n]."""
+    scales and bias fp32; y fp32 (default), fp16 or bf16 [T][n].  Results that a bounded wait which ran out kept from being computed are NaN;
+    dev_status (torch.int32[1] on the device, zeroed, or None) then becomes STB_ERR_TIMEOUT."""
     return (_bind or _fast()).gemm_i8(xq, x_scale, wq, w_scale, bias, out, out_dtype, dev_status, stream)
 
 
-def _gemm_i8_py(xq, x_scale, wq, w_scale, bias=None, out=None, out_dtype=None, dev_status=None, stream=None):
+def gemm_i8_wait_selftest(xq, x_scale, wq, w_scale, out, dev_status, bias=None, stream=None):
+    """stb_gemm_i8_wait_selftest: the product with some of its copies off and a short wait limit; dev_status (torch.int32[1], zeroed) becomes
+    STB_ERR_TIMEOUT, results without those copies NaN."""
+    return _gemm_i8_py(xq, x_scale, wq, w_scale, bias, out, None, dev_status, stream, _lib.stb_gemm_i8_wait_selftest)
+
+
+def _gemm_i8_py(xq, x_scale, wq, w_scale, bias=None, out=None, out_dtype=None, dev_status=None, stream=None, entry=None):
     import torch
     xr, wr = _rows(xq, xq, "gemm_i8: xq"), _rows(wq, xq, "gemm_i8: wq")
     T, m = xr.shape
@@ -586,7 +594,7 @@ def _gemm_i8_py(xq, x_scale, wq, w_scale, bias=None, out=None, out_dtype=None, d
             _result(stream, made)
         y = made if out is None else _rows(out, xq, "gemm_i8: out")
         _refuse(y.shape != (T, n), "gemm_i8: out")
-        _check(_lib.stb_gemm_i8(_ptr(wr), _ld(wr, 16), _ptr(w_scale), _ptr(bias), n, m, _ptr(xr), _ld(xr, 16), _ptr(x_scale), T, _ptr(y),
+        _check((entry or _lib.stb_gemm_i8)(_ptr(wr), _ld(wr, 16), _ptr(w_scale), _ptr(bias), n, m, _ptr(xr), _ld(xr, 16), _ptr(x_scale), T, _ptr(y),
                                 _dtype(y.dtype, "gemm_i8: out"), _ld(y), _ptr(dev_status), _launch_stream(stream, xq)), "stb_gemm_i8")
     return out if out is not None else (y if xq.dim() == 2 else y[0])
 

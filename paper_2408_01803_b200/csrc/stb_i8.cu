@@ -16,6 +16,9 @@ namespace cg = cooperative_groups;
 
 namespace stb {
 
+// A wait that runs out ends its CTA's part of the call: the results that are then not known become NaN, so that nobody takes them for results, and *dev_status, where
+// there is one, STB_ERR_TIMEOUT.  Self-test: copies off for some of the CTAs or tiles, and a limit of about 50 microseconds.
+constexpr long long kI8SelftestLimit = 100000;
 constexpr int kI8MaxSide = 1 << 30;      // of n and T: tiles and what lies behind the last one are counted in 32 bits
 
 struct I8Args {
@@ -206,7 +209,10 @@ __device__ __forceinline__ void i8_channel_out(const I8Args& a, const uint32_t (
 // ks = 1: straight to Y.  Else eight tokens at a time belong to one CTA of the cluster (group of eight mod ks), which gets everybody's sums of them
 // into its shared memory (32 bytes per channel and CTA), adds, scales and stores.  Bound by HBM where W is large (28672 x 8192, one token 38.7 us, 94 % of its
 // bytes' time; 4096 x 11008, 64 tokens, 11.1 us: 64 %, the rest the way from the launch to the first stage and the sum of the cluster).
-struct I8Batch { int lks, per, stages, ttiles, bn, ring, prefetch; uint32_t stage_bytes, tmem; };
+// A CTA without its sums hands over kI8Lost in their place, which no sum of a part of K is (|sum| < 2^31).
+// `off`: the part of K that is not copied (self-test), else -1.
+struct I8Batch { int lks, per, stages, ttiles, bn, ring, prefetch, off; uint32_t stage_bytes, tmem; long long limit; };
+constexpr uint32_t kI8Lost = 0x80000000u;
 constexpr int kI8BatchThreads = 256;
 constexpr uint32_t kI8BatchScale = 1024, kI8BatchRing = 2048;     // the tokens' scales; the ring, and behind it the sums that the CTAs hand over
 constexpr int kI8MaxRing = 12;
@@ -250,8 +256,8 @@ gemm_i8_batch_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_cons
     int s = 0;
     uint32_t parity = 1;
     for (int it = 0; it < count; ++it) {
-      if (!__all_sync(0xFFFFFFFFu, gemm_wait(bar_empty + 8 * s, parity, abort_flag))) break;
-      if (leader) {
+      if (!__all_sync(0xFFFFFFFFu, gemm_wait(bar_empty + 8 * s, parity, abort_flag, sh.limit))) break;
+      if (leader && kz != sh.off) {
         const uint32_t at = sbase + kI8BatchRing + (uint32_t)s * sh.stage_bytes, full = bar_full + 8 * s;
         mbar_expect_tx(full, sh.stage_bytes);
         tma_load_2d(at, &wmap, (s0 + it) * kI8K, mt * kI8M, full);
@@ -268,10 +274,10 @@ gemm_i8_batch_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_cons
     const bool leader = elect_one();
     const uint32_t desc_hi = (uint32_t)(umma_desc(0u) >> 32), lo0 = (uint32_t)umma_desc(sbase + kI8BatchRing), idesc = i8_idesc(kI8M, sh.bn);
     const uint32_t tmem_u = __shfl_sync(0xFFFFFFFFu, tmem_d, 0);
-    int s = 0;
+    int s = 0, it = 0;
     uint32_t parity = 0;
-    for (int it = 0; it < count; ++it) {
-      if (!__all_sync(0xFFFFFFFFu, gemm_wait(bar_full + 8 * s, parity, abort_flag))) break;
+    for (; it < count; ++it) {
+      if (!__all_sync(0xFFFFFFFFu, gemm_wait(bar_full + 8 * s, parity, abort_flag, sh.limit))) break;
       tc_fence_after();
       const uint32_t a_lo = lo0 + (uint32_t)s * (sh.stage_bytes >> 4), b_lo = a_lo + (kI8StageA >> 4);
       if (leader) {
@@ -282,60 +288,63 @@ gemm_i8_batch_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_cons
       __syncwarp();
       if (++s == sh.ring) { s = 0; parity ^= 1u; }
     }
-    if (leader) umma_commit(bar_accum);
+    if (leader && it >= count) umma_commit(bar_accum);                  // (sums of fewer stages are nobody's: the waits for them run out)
     __syncwarp();
   }
-  const bool have = __all_sync(0xFFFFFFFFu, gemm_wait(bar_accum, 0u, abort_flag));
+  const bool have = __all_sync(0xFFFFFFFFu, gemm_wait(bar_accum, 0u, abort_flag, sh.limit));
   tc_fence_after();
   const uint32_t from = tmem_d + ((uint32_t)(32 * (warp & 3)) << 16);
   const float* scales = reinterpret_cast<const float*>(smem + kI8BatchScale);
   const int live = min(sh.bn, args.T - tt * sh.bn);                    // tokens of the tile
   if (ks == 1) {
     __syncthreads();                                                   // (the scales)
-    if (have) {
-      for (int c0 = 32 * half; c0 < live; c0 += 64) {
-        uint32_t v[32];
+    for (int c0 = 32 * half; c0 < live; c0 += 64) {
+      uint32_t v[32];
+      if (have) {
         tmem_ask32(from + (uint32_t)c0, v);
         tmem_wait32(v);
-        if (r < args.n) i8_channel_out<32>(args, v, scales + c0, ws, b, bias != nullptr, tt * sh.bn + c0, live - c0, r);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = 0u;
       }
+      if (r < args.n) i8_channel_out<32>(args, v, scales + c0, have ? ws : __uint_as_float(0x7FC00000u), b, bias != nullptr, tt * sh.bn + c0, live - c0, r);
     }
   } else {
     cluster_wait();
-    if (have) {
-      const uint32_t mine = sbase + kI8BatchRing + (uint32_t)sh.ring * sh.stage_bytes + (uint32_t)(kz * kI8M) * 32u + (uint32_t)row * 16u;
-      for (int c0 = 32 * half; c0 < live; c0 += 64) {
-        uint32_t v[32];
-        if (count > 0) {
-          tmem_ask32(from + (uint32_t)c0, v);
-          tmem_wait32(v);
-        } else {
+    const uint32_t mine = sbase + kI8BatchRing + (uint32_t)sh.ring * sh.stage_bytes + (uint32_t)(kz * kI8M) * 32u + (uint32_t)row * 16u;
+    for (int c0 = 32 * half; c0 < live; c0 += 64) {
+      uint32_t v[32];
+      if (have && count > 0) {
+        tmem_ask32(from + (uint32_t)c0, v);
+        tmem_wait32(v);
+      } else {
 #pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] = 0u;                      // (no columns of K were left for this CTA)
-        }
+        for (int i = 0; i < 32; ++i) v[i] = have ? 0u : kI8Lost;       // (have: no columns of K were left for this CTA)
+      }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int g = (c0 >> 3) + j;
-          if (8 * g >= live) break;
-          const uint32_t to = smem_of_rank(mine + (uint32_t)((g >> lks << lks) * kI8M) * 32u, (uint32_t)(g & (ks - 1)));
-          asm volatile("st.shared::cluster.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(v[8 * j]), "r"(v[8 * j + 1]), "r"(v[8 * j + 2]), "r"(v[8 * j + 3]) : "memory");
-          asm volatile("st.shared::cluster.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to + 16u * kI8M), "r"(v[8 * j + 4]), "r"(v[8 * j + 5]), "r"(v[8 * j + 6]), "r"(v[8 * j + 7]) : "memory");
-        }
+      for (int j = 0; j < 4; ++j) {
+        const int g = (c0 >> 3) + j;
+        if (8 * g >= live) break;
+        const uint32_t to = smem_of_rank(mine + (uint32_t)((g >> lks << lks) * kI8M) * 32u, (uint32_t)(g & (ks - 1)));
+        asm volatile("st.shared::cluster.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(v[8 * j]), "r"(v[8 * j + 1]), "r"(v[8 * j + 2]), "r"(v[8 * j + 3]) : "memory");
+        asm volatile("st.shared::cluster.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to + 16u * kI8M), "r"(v[8 * j + 4]), "r"(v[8 * j + 5]), "r"(v[8 * j + 6]), "r"(v[8 * j + 7]) : "memory");
       }
     }
     cluster_arrive();
     cluster_wait();
-    if (have && r < args.n) {
+    if (r < args.n) {
       const uint8_t* sums = smem + kI8BatchRing + (size_t)sh.ring * sh.stage_bytes + (size_t)row * 16;
       for (int g = half * ks + kz; 8 * g < live; g += 2 * ks) {
         uint32_t v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        bool lost = false;
 #pragma unroll 4
         for (int z = 0; z < ks; ++z) {
           const uint4* p = reinterpret_cast<const uint4*>(sums + (size_t)((g >> lks << lks) + z) * (kI8M * 32));
           const uint4 lo = p[0], hi = p[kI8M];
+          lost = lost || lo.x == kI8Lost;
           v[0] += lo.x; v[1] += lo.y; v[2] += lo.z; v[3] += lo.w; v[4] += hi.x; v[5] += hi.y; v[6] += hi.z; v[7] += hi.w;
         }
-        i8_channel_out<8>(args, v, scales + 8 * g, ws, b, bias != nullptr, tt * sh.bn + 8 * g, live - 8 * g, r);
+        i8_channel_out<8>(args, v, scales + 8 * g, lost ? __uint_as_float(0x7FC00000u) : ws, b, bias != nullptr, tt * sh.bn + 8 * g, live - 8 * g, r);
       }
     }
   }
@@ -435,7 +444,7 @@ static cudaError_t launch_cluster(const void* kernel, unsigned grid, unsigned cl
   return cudaLaunchKernelExC(&cfg, kernel, params);
 }
 
-static int launch_i8_batch(const I8Args& a, const I8Plan& plan, int* dev_status, cudaStream_t s) {
+static int launch_i8_batch(const I8Args& a, const I8Plan& plan, int* dev_status, cudaStream_t s, bool selftest) {
   EncodeTiledFn enc = encode_tiled_fn();
   if (!enc) return STB_ERR_CUDA;
   I8Batch sh;
@@ -450,6 +459,8 @@ static int launch_i8_batch(const I8Args& a, const I8Plan& plan, int* dev_status,
   sh.ring = i8_ring(sh.bn, ks, plan.half);
   sh.prefetch = ctas <= (plan.half ? 296 : 148) ? 4 : 0;       // (a CTA that starts late has nobody to hide behind)
   sh.tmem = sh.bn <= 32 ? 32 : (sh.bn <= 64 ? 64 : (sh.bn <= 128 ? 128 : 256));
+  sh.off = selftest ? (sh.stages - 1) / sh.per : -1;           // (the last part that has columns)
+  sh.limit = selftest ? kI8SelftestLimit : kGemmWaitLimit;
   const uint32_t smem = kI8BatchRing + (uint32_t)sh.ring * sh.stage_bytes + sums;
   CUtensorMap wmap, xmap;
   if (!i8_map(enc, &wmap, a.W, a.n, a.m, a.ldw, kI8M) || !i8_map(enc, &xmap, a.X, a.T, a.m, a.ldx, sh.bn)) return STB_ERR_ARG;
@@ -470,7 +481,8 @@ static int launch_i8_batch(const I8Args& a, const I8Plan& plan, int* dev_status,
 //   warp 0 brings the stages, warp 1 issues the products, warps 4 to 7 read the sums out: 32 tokens at a time through shared memory, from where they leave
 //   as rows of 128 channels by TMA.  A TMA store writes whole 16-byte pieces, the last one beyond n as zeros: it takes the first `whole` channels, a multiple
 //   of such a piece, and plain stores the rest (or all, where rows of Y are on no 16-byte boundary: whole = 0).
-struct I8Prefill { int stages, ttiles, tiles, bn, ring, whole; uint32_t stage_bytes; };
+// `copied`: the tiles from this one on are not copied (self-test).
+struct I8Prefill { int stages, ttiles, tiles, bn, ring, whole, copied; uint32_t stage_bytes; long long limit; };
 constexpr int kI8PrefillThreads = 256, kI8PrefillMaxRing = 10, kI8OutTokens = 32;
 constexpr uint32_t kI8OutBytes = kI8OutTokens * kI8M * 4u;
 constexpr uint32_t kI8PrefillScale = 512, kI8PrefillOut = 2048, kI8PrefillRing = kI8PrefillOut + 2u * kI8OutBytes;      // (a tile's scales: 256 floats)
@@ -484,14 +496,14 @@ __device__ __forceinline__ void umma_commit_pair(uint32_t bar) {      // arrives
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort_flag) {      // gemm_wait for arrivals of the other CTA
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit) {      // gemm_wait for arrivals of the other CTA
   const long long t0 = clock64();
   for (;;) {
     uint32_t ok;
     asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     if (ok) return true;
     if (*abort_flag) return false;
-    if (clock64() - t0 > kGemmWaitLimit) { *abort_flag = 1; return false; }
+    if (clock64() - t0 > limit) { *abort_flag = 1; return false; }
   }
 }
 // A channel's results for 32 tokens, into rows of 128 channels in shared memory.
@@ -564,9 +576,9 @@ gemm_i8_prefill_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_co
     for (int tile = first; tile < sh.tiles && ok; tile += step) {
       const int wrow = (tile / sh.ttiles) * 2 * kI8M + rank * kI8M, xrow = (tile % sh.ttiles) * sh.bn + rank * (sh.bn >> 1);
       for (int it = 0; it < sh.stages; ++it) {
-        ok = __all_sync(0xFFFFFFFFu, gemm_wait(bar_empty + 8 * s, parity, abort_flag));
+        ok = __all_sync(0xFFFFFFFFu, gemm_wait(bar_empty + 8 * s, parity, abort_flag, sh.limit));
         if (!ok) break;
-        if (leader) {
+        if (leader && tile < sh.copied) {
           const uint32_t at = sbase + kI8PrefillRing + (uint32_t)s * sh.stage_bytes;
           if (rank == 0) mbar_expect_tx(bar_full + 8 * s, 2u * sh.stage_bytes);
           tma_load_2d_pair(at, &wmap, it * kI8K, wrow, full0 + 8 * s);
@@ -578,7 +590,7 @@ gemm_i8_prefill_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_co
     }
     // the first CTA's products signal this one's barriers: all of that has arrived before the CTA may leave
     for (int i = 0; i < sh.ring && ok; ++i) {
-      ok = __all_sync(0xFFFFFFFFu, gemm_wait(bar_empty + 8 * s, parity, abort_flag));
+      ok = __all_sync(0xFFFFFFFFu, gemm_wait(bar_empty + 8 * s, parity, abort_flag, sh.limit));
       if (++s == sh.ring) { s = 0; parity ^= 1u; }
     }
     if (*abort_flag) {       // let copies in flight land before the CTA gives its shared memory up
@@ -594,11 +606,11 @@ gemm_i8_prefill_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_co
     bool ok = true;
     for (int tile = first; tile < sh.tiles && ok; tile += step, ++use) {
       const int acc = use & 1;
-      ok = __all_sync(0xFFFFFFFFu, mbar_wait_cluster(bar_acc_empty + 8 * acc, ((uint32_t)(use >> 1) & 1u) ^ 1u, abort_flag));
+      ok = __all_sync(0xFFFFFFFFu, mbar_wait_cluster(bar_acc_empty + 8 * acc, ((uint32_t)(use >> 1) & 1u) ^ 1u, abort_flag, sh.limit));
       if (!ok) break;
       tc_fence_after();
       for (int it = 0; it < sh.stages; ++it) {
-        ok = __all_sync(0xFFFFFFFFu, gemm_wait(bar_full + 8 * s, parity, abort_flag));
+        ok = __all_sync(0xFFFFFFFFu, gemm_wait(bar_full + 8 * s, parity, abort_flag, sh.limit));
         if (!ok) break;
         tc_fence_after();
         const uint32_t a_lo = lo0 + (uint32_t)s * (sh.stage_bytes >> 4), b_lo = a_lo + (kI8StageA >> 4);
@@ -610,7 +622,7 @@ gemm_i8_prefill_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_co
         __syncwarp();
         if (++s == sh.ring) { s = 0; parity ^= 1u; }
       }
-      if (leader) umma_commit_pair(bar_acc_full + 8 * acc);      // (also where the loop was left early: the sums are then not used)
+      if (leader && ok) umma_commit_pair(bar_acc_full + 8 * acc);      // (sums of fewer stages are nobody's: the waits for them run out)
       __syncwarp();
     }
   } else if (warp >= 4) {
@@ -618,13 +630,13 @@ gemm_i8_prefill_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_co
     const uint32_t acc_empty0 = smem_of_rank(bar_acc_empty, 0u);
     const int elem = args.ydt == STB_F32 ? 4 : 2;
     float* scales = reinterpret_cast<float*>(smem + kI8PrefillScale);
-    int use = 0, buf = 0;
-    for (int tile = first; tile < sh.tiles; tile += step, ++use) {
+    int use = 0, buf = 0, tile = first;
+    for (; tile < sh.tiles; tile += step, ++use) {
       const int acc = use & 1, r0 = (tile / sh.ttiles) * 2 * kI8M + rank * kI8M, r = r0 + row, tok0 = (tile % sh.ttiles) * sh.bn;
       const float ws = r < args.n ? w_scale[r] : 0.0f, b = bias && r < args.n ? bias[r] : 0.0f;
       asm volatile("bar.sync 1, 128;" ::: "memory");             // the last tile's scales have been read
       for (int i = t128; i < sh.bn; i += 128) scales[i] = tok0 + i < args.T ? x_scale[tok0 + i] : 0.0f;
-      if (!barrier_and(gemm_wait(bar_acc_full + 8 * acc, (uint32_t)(use >> 1) & 1u, abort_flag))) break;      // (one verdict for the four warps)
+      if (!barrier_and(gemm_wait(bar_acc_full + 8 * acc, (uint32_t)(use >> 1) & 1u, abort_flag, sh.limit))) break;      // (one verdict for the four warps)
       tc_fence_after();
       uint32_t even[32], odd[32];
       const uint32_t from = tmem_d + ((uint32_t)(32 * q) << 16) + 256u * acc;
@@ -669,6 +681,11 @@ gemm_i8_prefill_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_co
       if (lane == 0) mbar_arrive_cluster(acc_empty0 + 8 * acc);
     }
     if (t128 == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    for (; tile < sh.tiles; tile += step) {                      // tiles without their sums
+      const int r = (tile / sh.ttiles) * 2 * kI8M + rank * kI8M + row, tok0 = (tile % sh.ttiles) * sh.bn;
+      if (r < args.n)
+        for (int t = tok0; t < min(tok0 + sh.bn, args.T); ++t) i8_store(args.Y, (size_t)t * args.ldy + r, args.ydt, __uint_as_float(0x7FC00000u));
+    }
   }
   tc_fence_before();
   __syncthreads();
@@ -681,7 +698,7 @@ gemm_i8_prefill_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_co
   if (threadIdx.x == 0 && *abort_flag && dev_status) *dev_status = STB_ERR_TIMEOUT;
 }
 
-static int launch_i8_prefill(const I8Args& a, const I8Plan& plan, int* dev_status, cudaStream_t s) {
+static int launch_i8_prefill(const I8Args& a, const I8Plan& plan, int* dev_status, cudaStream_t s, bool selftest) {
   EncodeTiledFn enc = encode_tiled_fn();
   if (!enc) return STB_ERR_CUDA;
   I8Prefill sh;
@@ -690,6 +707,9 @@ static int launch_i8_prefill(const I8Args& a, const I8Plan& plan, int* dev_statu
   const long long tiles = (long long)((a.n + 2 * kI8M - 1) / (2 * kI8M)) * sh.ttiles;
   if (tiles > 0x7FFFFFFF) return STB_ERR_SHAPE;
   sh.tiles = (int)tiles;
+  const int pairs = sh.tiles < 74 ? sh.tiles : 74;
+  sh.copied = !selftest ? sh.tiles : (sh.tiles > pairs ? pairs : 0);      // (self-test: a pair's first tile, where it has more)
+  sh.limit = selftest ? kI8SelftestLimit : kGemmWaitLimit;
   sh.stage_bytes = kI8StageA + (uint32_t)sh.bn * (kI8K / 2);
   sh.ring = (int)((kI8SmemMax - kI8PrefillRing) / sh.stage_bytes);
   if (sh.ring > kI8PrefillMaxRing) sh.ring = kI8PrefillMaxRing;
@@ -710,14 +730,13 @@ static int launch_i8_prefill(const I8Args& a, const I8Plan& plan, int* dev_statu
   if (allow_smem(reinterpret_cast<const void*>(gemm_i8_prefill_kernel), done, kI8SmemMax) != cudaSuccess) return STB_ERR_CUDA;
   I8Args args = a;
   void* params[] = {&wmap, &xmap, &ymap, &args, &sh, &dev_status};
-  const int pairs = sh.tiles < 74 ? sh.tiles : 74;
   return launch_cluster(reinterpret_cast<const void*>(gemm_i8_prefill_kernel), 2u * (unsigned)pairs, 2u, kI8PrefillThreads, smem, s, params) == cudaSuccess ? STB_OK : STB_ERR_CUDA;
 }
 
 }  // namespace stb
 
-extern "C" int stb_gemm_i8(const int8_t* W, size_t ldw, const float* w_scale, const float* bias, int n, int m, const int8_t* X, size_t ldx,
-                           const float* x_scale, int T, void* Y, stb_dtype ydt, size_t ldy, int* dev_status, void* stream) {
+static int gemm_i8_impl(const int8_t* W, size_t ldw, const float* w_scale, const float* bias, int n, int m, const int8_t* X, size_t ldx,
+                        const float* x_scale, int T, void* Y, stb_dtype ydt, size_t ldy, int* dev_status, void* stream, bool selftest) {
   if (!W || !w_scale || !X || !x_scale || !Y) return STB_ERR_ARG;
   if (n < 1 || m < 1 || T < 1 || m > 131071 || n > stb::kI8MaxSide || T > stb::kI8MaxSide) return STB_ERR_SHAPE;
   if (ydt != STB_F32 && ydt != STB_F16 && ydt != STB_BF16) return STB_ERR_UNSUPPORTED;
@@ -728,7 +747,18 @@ extern "C" int stb_gemm_i8(const int8_t* W, size_t ldw, const float* w_scale, co
     return STB_ERR_ARG;
   const stb::I8Args a = {W, X, w_scale, bias, x_scale, Y, ldw, ldx, ldy, n, m, T, ydt};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (const int ksplit = stb::gemv_i8_split(n, m, T)) return stb::launch_gemv_i8(a, ksplit, s) == cudaSuccess ? STB_OK : STB_ERR_CUDA;
+  if (const int ksplit = stb::gemv_i8_split(n, m, T)) return selftest ? STB_ERR_UNSUPPORTED : stb::launch_gemv_i8(a, ksplit, s) == cudaSuccess ? STB_OK : STB_ERR_CUDA;
   const stb::I8Plan plan = stb::i8_plan(n, m, T);
-  return plan.pair ? stb::launch_i8_prefill(a, plan, dev_status, s) : stb::launch_i8_batch(a, plan, dev_status, s);
+  return plan.pair ? stb::launch_i8_prefill(a, plan, dev_status, s, selftest) : stb::launch_i8_batch(a, plan, dev_status, s, selftest);
+}
+
+extern "C" int stb_gemm_i8(const int8_t* W, size_t ldw, const float* w_scale, const float* bias, int n, int m, const int8_t* X, size_t ldx,
+                           const float* x_scale, int T, void* Y, stb_dtype ydt, size_t ldy, int* dev_status, void* stream) {
+  return gemm_i8_impl(W, ldw, w_scale, bias, n, m, X, ldx, x_scale, T, Y, ydt, ldy, dev_status, stream, false);
+}
+
+extern "C" int stb_gemm_i8_wait_selftest(const int8_t* W, size_t ldw, const float* w_scale, const float* bias, int n, int m, const int8_t* X, size_t ldx,
+                                         const float* x_scale, int T, void* Y, stb_dtype ydt, size_t ldy, int* dev_status, void* stream) {
+  if (!dev_status) return STB_ERR_ARG;
+  return gemm_i8_impl(W, ldw, w_scale, bias, n, m, X, ldx, x_scale, T, Y, ydt, ldy, dev_status, stream, true);
 }

@@ -58,13 +58,13 @@ __device__ __forceinline__ uint64_t umma_desc(uint32_t smem_addr) {
 // single-lane roles back off between polls so that their spinning does not take issue slots from
 // the decode warps that share their schedulers.
 template <bool kBackoff = false>
-__device__ __forceinline__ bool gemm_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+__device__ __forceinline__ bool gemm_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit = kGemmWaitLimit) {
   if (mbar_try_wait(bar, parity)) return true;
   const long long t0 = clock64();
   while (!mbar_try_wait(bar, parity)) {
     if (kBackoff) __nanosleep(32);
     if (*abort_flag) return false;
-    if (clock64() - t0 > kGemmWaitLimit) { *abort_flag = 1; return false; }
+    if (clock64() - t0 > limit) { *abort_flag = 1; return false; }
   }
   return true;
 }
