@@ -479,10 +479,10 @@ static int launch_i8_batch(const I8Args& a, const I8Plan& plan, int* dev_status,
 // multiply-adds of the pair: at bn = 256 64 bytes per clock of the tensor core, what an SM gets from L2.  28672 x 8192, 2048 tokens, 282 us: 3.4 POP/s (3.0 once the
 // GPU is at its power limit).
 //   warp 0 brings the stages, warp 1 issues the products, warps 4 to 7 read the sums out: 32 tokens at a time through shared memory, from where they leave
-//   as rows of 128 channels by TMA.  A TMA store writes whole 16-byte pieces, the last one beyond n as zeros: it takes the first `whole` channels, a multiple
-//   of such a piece, and plain stores the rest (or all, where rows of Y are on no 16-byte boundary: whole = 0).
+//   as rows of 128 channels by TMA, or by plain stores where rows of Y are on no 16-byte boundary or n ends inside a piece of 16 bytes (TMA writes whole pieces: what lies
+//   behind the n-th value would become zeros).
 // `copied`: the tiles from this one on are not copied (self-test).
-struct I8Prefill { int stages, ttiles, tiles, bn, ring, whole, copied; uint32_t stage_bytes; long long limit; };
+struct I8Prefill { int stages, ttiles, tiles, bn, ring, tma_out, copied; uint32_t stage_bytes; long long limit; };
 constexpr int kI8PrefillThreads = 256, kI8PrefillMaxRing = 10, kI8OutTokens = 32;
 constexpr uint32_t kI8OutBytes = kI8OutTokens * kI8M * 4u;
 constexpr uint32_t kI8PrefillScale = 512, kI8PrefillOut = 2048, kI8PrefillRing = kI8PrefillOut + 2u * kI8OutBytes;      // (a tile's scales: 256 floats)
@@ -638,43 +638,43 @@ gemm_i8_prefill_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_co
       for (int i = t128; i < sh.bn; i += 128) scales[i] = tok0 + i < args.T ? x_scale[tok0 + i] : 0.0f;
       if (!barrier_and(gemm_wait(bar_acc_full + 8 * acc, (uint32_t)(use >> 1) & 1u, abort_flag, sh.limit))) break;      // (one verdict for the four warps)
       tc_fence_after();
-      uint32_t even[32], odd[32];
+      uint32_t v[2][32];
       const uint32_t from = tmem_d + ((uint32_t)(32 * q) << 16) + 256u * acc;
-      // Only chunks that hold a result are read and written, none where all 128 channels lie behind n.  Every chunk closes one group of stores (an empty one where TMA has
-      // no channel of it), so that "all but the newest group" is every use of the buffer that a chunk takes: the buffers alternate with the groups, from tile to tile too.
-      const int live = r0 < args.n ? min(sh.bn, args.T - tok0) : 0;
-      auto chunk = [&](int c0, uint32_t (&now)[32], uint32_t (&next)[32]) {
+      tmem_ask32(from, v[0]);
+      // Each chunk of 32 tokens takes the other buffer and closes one group of stores, an empty one where it lies behind the last token or channel: "all but the newest
+      // group" is then every earlier use of the chunk's buffer, from tile to tile too.
+#pragma unroll 2
+      for (int c0 = 0; c0 < sh.bn; c0 += kI8OutTokens, buf ^= 1) {
+        uint32_t(&now)[32] = v[(c0 / kI8OutTokens) & 1];
         tmem_wait32(now);
-        if (c0 + kI8OutTokens < live) tmem_ask32(from + (uint32_t)(c0 + kI8OutTokens), next);
+        if (c0 + kI8OutTokens < sh.bn) tmem_ask32(from + (uint32_t)(c0 + kI8OutTokens), v[((c0 / kI8OutTokens) & 1) ^ 1]);
         const uint32_t out = sbase + kI8PrefillOut + (uint32_t)buf * kI8OutBytes;
-        if (t128 == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");       // the store before last, this buffer's, has read it
+        if (t128 == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");       // the group before last, this buffer's, has been read
         asm volatile("bar.sync 1, 128;" ::: "memory");             // (plain stores: each thread reads back what it alone has written)
         switch (args.ydt) {
           case STB_F32: i8_rows_out<STB_F32>(now, scales + c0, ws, b, bias != nullptr, out, row); break;
           case STB_F16: i8_rows_out<STB_F16>(now, scales + c0, ws, b, bias != nullptr, out, row); break;
           default: i8_rows_out<STB_BF16>(now, scales + c0, ws, b, bias != nullptr, out, row); break;
         }
-        if (r0 < sh.whole) fence_async_smem();
+        if (sh.tma_out) fence_async_smem();
         asm volatile("bar.sync 1, 128;" ::: "memory");
-        if (t128 == 0) {
-          if (r0 < sh.whole)
-            asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(&ymap), "r"(out), "r"(r0), "r"(tok0 + c0) : "memory");
-          asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        if (r0 >= args.n || tok0 + c0 >= args.T) {
+          if (t128 == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+          continue;
         }
-        if (r >= sh.whole && r < args.n) {
-          for (int i = 0; i < kI8OutTokens && c0 + i < live; ++i) {
+        if (sh.tma_out) {
+          if (t128 == 0) {
+            asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(&ymap), "r"(out), "r"(r0), "r"(tok0 + c0) : "memory");
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+          }
+        } else if (r < args.n) {
+          for (int i = 0; i < kI8OutTokens && tok0 + c0 + i < args.T; ++i) {
             const size_t at = (size_t)(tok0 + c0 + i) * args.ldy + r;
             const uint8_t* p = smem + kI8PrefillOut + (size_t)buf * kI8OutBytes + (size_t)(i * kI8M + row) * elem;
             if (elem == 4) static_cast<float*>(args.Y)[at] = *reinterpret_cast<const float*>(p);
             else static_cast<uint16_t*>(args.Y)[at] = *reinterpret_cast<const uint16_t*>(p);
           }
         }
-        buf ^= 1;
-      };
-      if (live > 0) tmem_ask32(from, even);
-      for (int c0 = 0; c0 < live; c0 += 2 * kI8OutTokens) {
-        chunk(c0, even, odd);
-        if (c0 + kI8OutTokens < live) chunk(c0 + kI8OutTokens, odd, even);
       }
       tc_fence_before();
       __syncwarp();
@@ -717,14 +717,13 @@ static int launch_i8_prefill(const I8Args& a, const I8Plan& plan, int* dev_statu
   CUtensorMap wmap, xmap, ymap = {};
   if (!i8_map(enc, &wmap, a.W, a.n, a.m, a.ldw, kI8M) || !i8_map(enc, &xmap, a.X, a.T, a.m, a.ldx, sh.bn / 2)) return STB_ERR_ARG;
   const int elem = a.ydt == STB_F32 ? 4 : 2;
-  sh.whole = (a.ldy * (size_t)elem) % 16 == 0 && (reinterpret_cast<uintptr_t>(a.Y) & 15u) == 0 ? a.n / (16 / elem) * (16 / elem) : 0;
-  if (sh.whole > 0) {
-    const cuuint64_t dims[2] = {(cuuint64_t)sh.whole, (cuuint64_t)a.T}, strides[1] = {(cuuint64_t)a.ldy * (cuuint64_t)elem};
+  sh.tma_out = (a.ldy * (size_t)elem) % 16 == 0 && ((size_t)a.n * (size_t)elem) % 16 == 0 && (reinterpret_cast<uintptr_t>(a.Y) & 15u) == 0;
+  if (sh.tma_out) {
+    const cuuint64_t dims[2] = {(cuuint64_t)a.n, (cuuint64_t)a.T}, strides[1] = {(cuuint64_t)a.ldy * (cuuint64_t)elem};
     const cuuint32_t box[2] = {(cuuint32_t)kI8M, (cuuint32_t)kI8OutTokens}, estr[2] = {1, 1};
     const CUtensorMapDataType dt = a.ydt == STB_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : (a.ydt == STB_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16);
-    if (enc(&ymap, dt, 2, a.Y, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_NONE,
-            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-      sh.whole = 0;
+    sh.tma_out = enc(&ymap, dt, 2, a.Y, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
   }
   static bool done[64] = {};
   if (allow_smem(reinterpret_cast<const void*>(gemm_i8_prefill_kernel), done, kI8SmemMax) != cudaSuccess) return STB_ERR_CUDA;
