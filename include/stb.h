@@ -316,8 +316,9 @@ typedef enum stb_norm_kind {
 /* What stb_block_norm does to every token (HOST struct; pointers to DEVICE memory, NULL = without that part):
  *   b = x;   if (post) b = norm(b) * post_weight + post_bias;   b = b * gate[t / tokens_per_gate];
  *   r = resid + alpha * b      -> resid_out
- *   v = norm(r) * weight + bias -> y (rounded to its type), and / or q, q_scale (v in 8 bits, as stb_quantize_i8 defines it)
- * in fp32 from the loads to the stores (r enters the second norm unrounded), sums over a row in fp32 in a fixed order. */
+ *   v = norm(r) * weight + bias -> y (rounded to its type), and / or q, q_scale (the fp32 values v in 8 bits, as stb_quantize_i8 defines it)
+ * in fp32 from the loads to the stores (r enters the second norm unrounded), sums over a row in fp32 in a fixed order.  The same call gives the same bits; but v
+ * is rounded on the way, so that q, unlike that of stb_quantize_i8, is not fixed by the definition: a value on a border between two whole numbers can go either way. */
 typedef struct stb_norm {
   int tokens, h;            /* h <= 32768, else STB_ERR_SIZE */
   stb_norm_kind kind;       /* of both norms */
@@ -345,7 +346,8 @@ typedef struct stb_norm {
 
 /* Norms before and after a block, fused with its gate, residual scale and residual sum: one pass over the tokens, one launch.  An output
  * may be the input of its type with the same leading dimension (resid_out = resid, y = x); otherwise outputs must not overlap anything.
- * Any alignment is taken; 16-byte rows (fp32: 32-byte, q: 8-byte) are the fast case.  (Squares of values beyond 10^19 overflow fp32: such a token is 0 or NaN.) */
+ * Any alignment is taken; 16-byte rows (fp32: 32-byte, q: 8-byte) are the fast case.  (Squares of values beyond 10^19 overflow fp32: such a token is 0 or
+ * NaN.  Those of values below 10^-19 lose digits and below 10^-23 vanish, which shows where eps is as small as they are.) */
 int stb_block_norm(const stb_norm *args, void *stream);
 
 /* Static string for a status code. */

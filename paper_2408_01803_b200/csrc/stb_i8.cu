@@ -370,7 +370,8 @@ __host__ inline int i8_ring(int bn, int ks, bool half) {
   return ring > kI8MaxRing ? kI8MaxRing : ring;
 }
 // The layout whose estimated time is smallest.  In microseconds, fitted to 4200 timed calls of 450 shapes (n, m of 64 to 28672, T of 1 to 4096); over them the choice
-// is 1.0 % behind the fastest layout of each shape on average, 4 % in one of ten.
+// is 1.0 % behind the fastest layout of each shape on average, 4 % in one of ten.  (The estimates rank layouts; as times they can be a third off: 33 for 24.7 at 5120 x 13824 and
+// 333 tokens.)
 //   gemm_i8_batch_kernel:   a stage of 128 columns 0.12 + 0.0014 bn (0.023 more where two CTAs share an SM), times the stages of the fullest SM; the bytes at
 //                           6.3 TB/s / 0.95, the tokens' rows counting 2.2 times (they are read by every row of tiles); the root of the sum of the two squared;
 //                           1.9 for the call, 0.019 bn per wave for reading the sums out, 0.7 for a cluster's sum, 2.5 per further wave

@@ -535,8 +535,8 @@ __device__ __forceinline__ uint32_t magnitude_bits(uint32_t m) {
   return __float_as_uint(a);
 }
 // kWarp: a row belongs to a warp, else to the CTA, which takes every gridDim-th one.  kAsync: the pieces of the next row are on their way.
-// Measured: 11008 x 4096 fp16 22.8 us (5.9 TB/s), 4096 x 28672 fp32 91 us (6.5 TB/s), bound by HBM; gated 2048 x 28672 bf16 72.5 us (4.1 TB/s), bound by issue
-// (28 instructions a value); 1 x 4096 1.6 us, the launch.
+// Measured: 11008 x 4096 fp16 22.8 us (5.9 TB/s), 4096 x 28672 fp32 91 us (6.5 TB/s), bound by HBM; gated 2048 x 28672 bf16 72.5 us (4.1 TB/s), bound by the way through a row:
+// one CTA of 896 threads an SM has nothing to issue around its barrier (issue active 63 %, no pipe above 50 %; 28 instructions a value); 1 x 4096 1.6 us, the launch.
 template <int P, int kType, bool kGated, bool kVec, bool kWarp, bool kAsync>
 __global__ void __launch_bounds__(kWarp ? 256 : (kAsync ? (kGated ? kMaxRowThreads : 512) : (!kVec && P > 2 ? 512 : kMaxRowThreads)),
                                   kWarp || (kAsync && !kGated && (P <= 4 || kType != STB_F32)) || (!kVec && P == 4) ? 2 : 1)
@@ -957,8 +957,9 @@ template <int kAll>
 static cudaError_t launch_norm(const stb_norm& a, const RowShape& s, bool vec, bool roomy, cudaStream_t st) {
   return vec ? launch_norm_as<kAll, true>(a, s, roomy, st) : launch_norm_as<kAll, false>(a, s, roomy, st);
 }
-// Whether the norms of rows on their way take 80 registers a thread (nothing is then spilled) or 64 (more rows at a time).  Tokens of mixed types: always
-// (2048 x 4096 with an fp32 residual 16.3 us against 19.0; 11008, layer norm with fp32 weights, 45 against 56; but 16384 77 against 70).  Of one type: where
+// Whether the norms of rows on their way take 80 registers a thread (nothing is then spilled, of mixed types 12 bytes) or 64 (more rows at a time).  Tokens of mixed types:
+// always (2048 x 4096 with an fp32 residual 16.3 us against 19.0; 11008, layer norm with fp32 weights, 45 against 56; 16384 loses, 77 against 70, which is not worth another set
+// of kernels; beyond 24576 values eight pieces a thread spill 280 bytes either way).  Of one type: where
 // more than three quarters as many threads fit an SM (2048 x 2816 8.1 us against 9.5, 22016 57.9 against 60.1, but 5120 14.2 against 13.0), or, with the norm
 // before the gate, as many as that (8192 27.6 against 28.2).
 static bool norm_roomy(int h, bool same, bool post) {
