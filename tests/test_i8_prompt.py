@@ -113,3 +113,41 @@ def test_product_of_many_tokens_at_the_ends_of_its_range(stb):
     y = stb.gemm_i8(x, one[:T], w, one[:n])
     want = torch.tensor([128.0 * 128 * m, -128.0 * 127 * m], dtype=torch.float64).float().cuda().repeat(n // 2)
     assert torch.equal(y, want.expand(T, n))
+
+
+@pytest.mark.gpu
+def test_products_of_many_tokens_captured_replayed_and_side_by_side(stb):
+    """Two graphs over the same weights, replayed on two streams at once with products of few tokens between them; inputs change between the replays."""
+    n, m, T = 4232, 640, 2100
+    wq, ws = _eight(n, m, 3)
+    ins = [_eight(T, m, 10 + k) for k in range(2)]
+    few = _eight(20, m, 30)
+    want = lambda x, s: torch.round(x.double() @ wq.double().T).float().mul_(s[:, None]).mul_(ws)  # noqa: E731
+    few_want = want(*few)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):                            # (every kernel has run once before it is captured)
+        stb.gemm_i8(*ins[0], wq, ws)
+        stb.gemm_i8(*few, wq, ws)
+    torch.cuda.synchronize()
+    graphs = []
+    for k in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = [stb.gemm_i8(*ins[k], wq, ws) for _ in range(3)] + [stb.gemm_i8(*few, wq, ws)]
+        graphs.append((g, out))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for seed in range(3):
+        for k in range(2):
+            x, s = _eight(T, m, 40 + 2 * seed + k)
+            ins[k][0].copy_(x)
+            ins[k][1].copy_(s)
+        torch.cuda.synchronize()
+        for _ in range(4):
+            for (g, _), s in zip(graphs, streams):
+                with torch.cuda.stream(s):
+                    g.replay()
+        torch.cuda.synchronize()
+        for k, (_, out) in enumerate(graphs):
+            w = want(*ins[k])
+            assert all(torch.equal(y, w) for y in out[:3]) and torch.equal(out[3], few_want)
